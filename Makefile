@@ -13,8 +13,9 @@ PYTHON ?= python3
 ARCH ?= gfx950
 PKG := paper_2510_13223_amd
 CSRC := $(PKG)/csrc
-SRCS := attn_partial.hip merge.hip migrate.hip validate.hip debug_rows.hip gather_read.hip scratch.hip bana_api.cpp
-HDRS := include/bana.h $(wildcard $(CSRC)/*.h)
+SRCS := attn_partial.hip merge.hip migrate.hip validate.hip debug_rows.hip gather_read.hip scratch.hip rows_attn.hip tokens.hip blocks.hip bana_api.cpp \
+        tokens_api.cpp
+HDRS := include/bana.h include/bana_tokens.h $(wildcard $(CSRC)/*.h)
 HIPFLAGS := --offload-arch=$(ARCH) -O3 -fPIC -std=c++17 -Wall -Xclang -target-feature -Xclang -packed-fp32-ops \
             -Iinclude -I$(CSRC)
 OBJ := _build/make
@@ -36,7 +37,7 @@ $(eval $(call hip_library,product,,$(PKG)/libbana.so))
 $(eval $(call hip_library,racecheck,-DBANA_LDS_RACE_CHECK,$(PKG)/libbana_racecheck.so))
 $(eval $(call hip_library,timeline,-DBANA_WAVE_TIMELINE,$(PKG)/libbana_timeline.so))
 
-$(PKG)/_native.so: $(CSRC)/binding.cpp include/bana.h
+$(PKG)/_native.so: $(CSRC)/binding.cpp include/bana.h include/bana_tokens.h
 	$(PYTHON) -c "from paper_2510_13223_amd import build; print(build.build_native())"
 
 oracle/liboracle.so: oracle/oracle.c

@@ -6,7 +6,8 @@ handle to the C ABI declared in ``include/bana.h``.  The calls of a decode
 step make these checks in ``_native`` (csrc/binding.cpp); where it finds
 anything not as wanted, the checks below run and say what.  All arithmetic runs in
 the library's HIP kernels; there is no fallback path, and a missing library
-raises.  PyTorch only provides device memory and streams.
+raises.  PyTorch only provides device memory and streams.  The calls on new
+tokens and on the cache's blocks (``include/bana_tokens.h``) are at the end.
 """
 
 from __future__ import annotations
@@ -89,7 +90,8 @@ def _calls():
             _native = _PythonChecks()
             return _native
         names = ("decode_attn_partial", "decode_attn_partial_noalloc", "decode_attn_fused", "decode_attn_fused_copies",
-                 "decode_attn_heads", "merge_partials", "migrate_kv_blocks")
+                 "decode_attn_heads", "merge_partials", "migrate_kv_blocks", "tree_attn", "window_attn", "append_kv",
+                 "compact_kv_tokens", "reserve_kv_blocks", "fork_kv_seqs", "release_kv_blocks")
         size = n.setup(tuple(ctypes.cast(getattr(L, "bana_" + name), ctypes.c_void_p).value for name in names),
                        torch._C._cuda_getCurrentRawStream, torch.cuda.Stream, bana_dims)
         if size != ctypes.sizeof(bana_dims):
@@ -146,6 +148,21 @@ def load(path: str) -> ctypes.CDLL:
     L.bana_debug_gather_read.restype = ctypes.c_int
     L.bana_debug_stream_read.argtypes = [P, ctypes.c_size_t, ctypes.c_int32, P, P]
     L.bana_debug_stream_read.restype = ctypes.c_int
+    I, R, S, F = ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float
+    for name, restype, argtypes in (
+            ("tree_attn", ctypes.c_int, [D, R, P, P, P, P, P, P, P, I, P, P, F, P, I, P, P, S, P]),
+            ("tree_attn_workspace_bytes", S, [D, R, I]),
+            ("window_attn", ctypes.c_int, [D, R, P, P, P, P, P, P, P, P, I, I, F, P, I, P, P, S, P]),
+            ("window_attn_workspace_bytes", S, [D, R, I, I]),
+            ("append_kv", ctypes.c_int, [D, R, P, P, P, P, P, P, P, P]),
+            ("compact_kv_tokens", ctypes.c_int, [D, P, P, P, P, P, I, P, P]),
+            ("reserve_kv_blocks", ctypes.c_int, [D, P, P, P, P, P, P, S, P]),
+            ("fork_kv_seqs", ctypes.c_int, [D, P, P, I, P, P, P, P, P, P, P, S, P]),
+            ("release_kv_blocks", ctypes.c_int, [D, P, P, P, P, P]),
+            ("kv_blocks_workspace_bytes", S, [D])):
+        f = getattr(L, "bana_" + name, None)  # absent where only the calls of bana.h are built
+        if f is not None:
+            f.argtypes, f.restype = argtypes, restype
     L.bana_debug_wave_timeline_clear.argtypes = [P]
     L.bana_debug_wave_timeline_clear.restype = ctypes.c_int
     L.bana_debug_wave_timeline_read.argtypes = [P, ctypes.c_size_t, P]
@@ -588,3 +605,237 @@ def bana_debug_wave_timeline_read(n_slots: int, stream=None, library: Optional[c
     if st != BANA_OK:
         raise BanaError(st, "bana_debug_wave_timeline_read")
     return out
+
+
+# ---- new tokens and the blocks of the cache (include/bana_tokens.h) --------------------------------
+
+_OUT_TYPES = {torch.float32: 0, torch.bfloat16: 1}  # BANA_OUT_F32, BANA_OUT_BF16
+
+
+def _check_pools(k_cache, v_cache, block_table):
+    """(batch, table width, num_blocks, Hkv) of a cache."""
+    if k_cache.dim() != 5:
+        raise ValueError("k_cache must be [num_blocks, Hkv, D / 8, block_size, 8]")
+    nb, Hkv = k_cache.shape[:2]
+    _need(k_cache, "k_cache", torch.bfloat16, (nb, Hkv, HEAD_DIM // 8, BLOCK_SIZE, 8))
+    _need(v_cache, "v_cache", torch.bfloat16, (nb, Hkv, HEAD_DIM, BLOCK_SIZE))
+    B, mb = _check_table(block_table)
+    return B, mb, nb, Hkv
+
+
+def _check_table(block_table):
+    _need(block_table, "block_table", torch.int32)
+    if block_table.dim() != 2:
+        raise ValueError("block_table must be [B, max_blocks_per_seq]")
+    return block_table.shape
+
+
+def _workspace_args(workspace):
+    if workspace is None:
+        return None, 0
+    _need(workspace, "workspace", workspace.dtype)
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def _check_rows(q, row_begin, k_cache, v_cache, block_table, out, lse, dims):
+    """What both attention calls on packed rows check: (dims, batch, rows, type of the result)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [rows, Hq, D]")
+    rows, Hq, D = q.shape
+    _need(q, "q", torch.bfloat16, (rows, Hq, HEAD_DIM))
+    B, mb, nb, Hkv = _check_pools(k_cache, v_cache, block_table)
+    _need(row_begin, "row_begin", torch.int32, (B + 1,))
+    if out.dtype not in _OUT_TYPES:
+        raise TypeError(f"out must be float32 or bfloat16, got {out.dtype}")
+    _need(out, "out", out.dtype, (rows, Hq, D))
+    if lse is not None:
+        _need(lse, "lse", torch.float32, (rows, Hq))
+    want = (B, Hq, Hkv, D, mb, nb)
+    if dims is None:
+        dims = bana_dims(B, Hq, Hkv, D, BLOCK_SIZE, mb, nb)
+    got = (dims.batch, dims.num_q_heads, dims.num_kv_heads, dims.head_dim, dims.max_blocks_per_seq, dims.num_blocks)
+    if got != want:
+        raise ValueError(f"dims (batch, Hq, Hkv, head_dim, max_blocks_per_seq, num_blocks) = {got} "
+                         f"do not match the tensors {want}")
+    return dims, B, rows, _OUT_TYPES[out.dtype]
+
+
+def bana_tree_attn(q, row_begin, k_cache, v_cache, block_table, kv_range_begin, kv_range_end, tree_begin, tree_mask,
+                   out, lse: Optional[torch.Tensor] = None, scale: float = 1.0,
+                   workspace: Optional[torch.Tensor] = None, stream=None, dims: Optional[bana_dims] = None) -> None:
+    """Attention of drafted tokens, the rows ``q [rows, Hq, D]``; see include/bana_tokens.h.
+
+    ``row_begin`` int32 [B + 1]; ``kv_range_begin`` / ``kv_range_end`` int32 [n_parts, B]; ``tree_begin`` int32 [B];
+    ``tree_mask`` int64 [rows], its bits those of a uint64; ``out`` float32 or bfloat16 like ``q``, ``lse`` float32
+    [rows, Hq] or None.  ``dims`` carries the length hints; its shapes must be those of the tensors.
+    """
+    st = _calls().tree(q, row_begin, k_cache, v_cache, block_table, kv_range_begin, kv_range_end, tree_begin,
+                       tree_mask, out, lse, scale, workspace, stream, dims)
+    if st is None:
+        dims, B, rows, kind = _check_rows(q, row_begin, k_cache, v_cache, block_table, out, lse, dims)
+        if kv_range_begin.dim() != 2 or kv_range_begin.shape[1] != B:
+            raise ValueError("kv_range_begin must be [n_parts, B]")
+        n = kv_range_begin.shape[0]
+        _need(kv_range_begin, "kv_range_begin", torch.int32, (n, B))
+        _need(kv_range_end, "kv_range_end", torch.int32, (n, B))
+        _need(tree_begin, "tree_begin", torch.int32, (B,))
+        _need(tree_mask, "tree_mask", torch.int64, (rows,))
+        _same_device(q, row_begin, k_cache, v_cache, block_table, kv_range_begin, kv_range_end, tree_begin, tree_mask,
+                     out, lse, workspace)
+        ws, ws_bytes = _workspace_args(workspace)
+        st = BANA_OK if rows == 0 else lib().bana_tree_attn(
+            ctypes.byref(dims), rows, _ptr(row_begin), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(kv_range_begin), _ptr(kv_range_end), n, _ptr(tree_begin), _ptr(tree_mask), float(scale), _ptr(out),
+            kind, _ptr(lse), ws, ws_bytes, _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_tree_attn")
+
+
+def bana_tree_attn_workspace_bytes(dims: bana_dims, rows: int, n_parts: int = 1) -> int:
+    return int(lib().bana_tree_attn_workspace_bytes(ctypes.byref(dims), rows, n_parts))
+
+
+def bana_window_attn(q, row_begin, k_cache, v_cache, block_table, seq_lens, window: int, sinks: int, out,
+                     lse: Optional[torch.Tensor] = None, scale: float = 1.0,
+                     kv_range_begin: Optional[torch.Tensor] = None, kv_range_end: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, stream=None, dims: Optional[bana_dims] = None) -> None:
+    """Attention of new tokens under a sliding window with ``sinks`` first tokens visible; see include/bana_tokens.h.
+
+    ``q [rows, Hq, D]`` packed by ``row_begin`` int32 [B + 1]; ``seq_lens`` int32 [B], new tokens included;
+    ``kv_range_begin`` / ``kv_range_end`` int32 [B] limit the call to one partition.  Others as ``bana_tree_attn``.
+    """
+    st = _calls().window(q, row_begin, k_cache, v_cache, block_table, seq_lens, window, sinks, out, lse, scale,
+                         kv_range_begin, kv_range_end, workspace, stream, dims)
+    if st is None:
+        dims, B, rows, kind = _check_rows(q, row_begin, k_cache, v_cache, block_table, out, lse, dims)
+        _need(seq_lens, "seq_lens", torch.int32, (B,))
+        if (kv_range_begin is None) != (kv_range_end is None):
+            raise ValueError("kv_range_begin and kv_range_end go together")
+        if kv_range_begin is not None:
+            _need(kv_range_begin, "kv_range_begin", torch.int32, (B,))
+            _need(kv_range_end, "kv_range_end", torch.int32, (B,))
+        if not 1 <= int(window) < 1 << 31 or not 0 <= int(sinks) < 1 << 31:
+            raise ValueError(f"window {window} must be positive, sinks {sinks} not negative, both 32-bit")
+        _same_device(q, row_begin, k_cache, v_cache, block_table, seq_lens, out, lse, kv_range_begin, kv_range_end,
+                     workspace)
+        ws, ws_bytes = _workspace_args(workspace)
+        st = BANA_OK if rows == 0 else lib().bana_window_attn(
+            ctypes.byref(dims), rows, _ptr(row_begin), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(seq_lens), _ptr(kv_range_begin), _ptr(kv_range_end), int(window), int(sinks), float(scale),
+            _ptr(out), kind, _ptr(lse), ws, ws_bytes, _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_window_attn")
+
+
+def bana_window_attn_workspace_bytes(dims: bana_dims, rows: int, window: int, sinks: int) -> int:
+    return int(lib().bana_window_attn_workspace_bytes(ctypes.byref(dims), rows, int(window), int(sinks)))
+
+
+def bana_append_kv(k_rows, v_rows, row_begin, first_token, block_table, k_cache, v_cache, stream=None) -> None:
+    """Keys and values ``[rows, Hkv, D]`` of new tokens into the cache; see include/bana_tokens.h."""
+    st = _calls().append(k_rows, v_rows, row_begin, first_token, block_table, k_cache, v_cache, stream)
+    if st is None:
+        B, mb, nb, Hkv = _check_pools(k_cache, v_cache, block_table)
+        if k_rows.dim() != 3:
+            raise ValueError("k_rows must be [rows, Hkv, D]")
+        rows = k_rows.shape[0]
+        _need(k_rows, "k_rows", torch.bfloat16, (rows, Hkv, HEAD_DIM))
+        _need(v_rows, "v_rows", torch.bfloat16, (rows, Hkv, HEAD_DIM))
+        _need(row_begin, "row_begin", torch.int32, (B + 1,))
+        _need(first_token, "first_token", torch.int32, (B,))
+        _same_device(k_rows, v_rows, row_begin, first_token, block_table, k_cache, v_cache)
+        dims = bana_dims(B, Hkv, Hkv, HEAD_DIM, BLOCK_SIZE, mb, nb)
+        st = BANA_OK if rows == 0 else lib().bana_append_kv(
+            ctypes.byref(dims), rows, _ptr(row_begin), _ptr(first_token), _ptr(k_rows), _ptr(v_rows),
+            _ptr(block_table), _ptr(k_cache), _ptr(v_cache), _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_append_kv")
+
+
+def bana_compact_kv_tokens(k_cache, v_cache, block_table, first_token, kept, n_kept, stream=None) -> None:
+    """Token ``first_token[b] + i`` of sequence b becomes ``first_token[b] + kept[b, i]``, i < ``n_kept[b]``, in
+    place; see include/bana_tokens.h."""
+    st = _calls().compact(k_cache, v_cache, block_table, first_token, kept, n_kept, stream)
+    if st is None:
+        B, mb, nb, Hkv = _check_pools(k_cache, v_cache, block_table)
+        _need(first_token, "first_token", torch.int32, (B,))
+        _need(kept, "kept", torch.int32)
+        if kept.dim() != 2 or kept.shape[0] != B:
+            raise ValueError("kept must be [B, max_kept]")
+        _need(n_kept, "n_kept", torch.int32, (B,))
+        _same_device(k_cache, v_cache, block_table, first_token, kept, n_kept)
+        dims = bana_dims(B, Hkv, Hkv, HEAD_DIM, BLOCK_SIZE, mb, nb)
+        st = BANA_OK if kept.shape[1] == 0 else lib().bana_compact_kv_tokens(
+            ctypes.byref(dims), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(first_token), _ptr(kept),
+            kept.shape[1], _ptr(n_kept), _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_compact_kv_tokens")
+
+
+def bana_kv_blocks_workspace_bytes(batch: int, max_blocks_per_seq: int, num_blocks: int) -> int:
+    """Bytes of workspace that bana_reserve_kv_blocks and bana_fork_kv_seqs need (0 for invalid sizes)."""
+    dims = bana_dims(batch, 1, 1, HEAD_DIM, BLOCK_SIZE, max_blocks_per_seq, num_blocks)
+    return int(lib().bana_kv_blocks_workspace_bytes(ctypes.byref(dims)))
+
+
+def _check_blocks(block_table, block_refs, status):
+    B, mb = _check_table(block_table)
+    _need(block_refs, "block_refs", torch.int32)
+    if block_refs.dim() != 1:
+        raise ValueError("block_refs must be [num_blocks]")
+    _need(status, "status", torch.int32, (1,))
+    return B, mb, block_refs.shape[0]
+
+
+def bana_reserve_kv_blocks(block_table, seq_lens, need_lens, block_refs, status, workspace, stream=None) -> None:
+    """Free blocks for the tokens ``[seq_lens[b], need_lens[b])`` of every sequence; see include/bana_tokens.h."""
+    st = _calls().reserve(block_table, seq_lens, need_lens, block_refs, status, workspace, stream)
+    if st is None:
+        B, mb, nb = _check_blocks(block_table, block_refs, status)
+        _need(seq_lens, "seq_lens", torch.int32, (B,))
+        _need(need_lens, "need_lens", torch.int32, (B,))
+        _same_device(block_table, seq_lens, need_lens, block_refs, status, workspace)
+        ws, ws_bytes = _workspace_args(workspace)
+        dims = bana_dims(B, 1, 1, HEAD_DIM, BLOCK_SIZE, mb, nb)
+        st = lib().bana_reserve_kv_blocks(ctypes.byref(dims), _ptr(block_table), _ptr(seq_lens), _ptr(need_lens),
+                                          _ptr(block_refs), _ptr(status), ws, ws_bytes, _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_reserve_kv_blocks")
+
+
+def bana_fork_kv_seqs(src_seq, dst_seq, k_cache, v_cache, block_table, seq_lens, block_refs, status, workspace,
+                      stream=None) -> None:
+    """Sequence ``dst_seq[i]`` becomes a copy of ``src_seq[i]``, sharing its whole blocks; see include/bana_tokens.h."""
+    st = _calls().fork(src_seq, dst_seq, k_cache, v_cache, block_table, seq_lens, block_refs, status, workspace, stream)
+    if st is None:
+        B, mb, nb, Hkv = _check_pools(k_cache, v_cache, block_table)
+        _check_blocks(block_table, block_refs, status)
+        _need(block_refs, "block_refs", torch.int32, (nb,))
+        _need(seq_lens, "seq_lens", torch.int32, (B,))
+        _need(src_seq, "src_seq", torch.int32)
+        if src_seq.dim() != 1:
+            raise ValueError("src_seq must be [n]")
+        n = src_seq.shape[0]
+        _need(dst_seq, "dst_seq", torch.int32, (n,))
+        _same_device(src_seq, dst_seq, k_cache, v_cache, block_table, seq_lens, block_refs, status, workspace)
+        ws, ws_bytes = _workspace_args(workspace)
+        dims = bana_dims(B, Hkv, Hkv, HEAD_DIM, BLOCK_SIZE, mb, nb)
+        st = BANA_OK if n == 0 else lib().bana_fork_kv_seqs(
+            ctypes.byref(dims), _ptr(src_seq), _ptr(dst_seq), n, _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+            _ptr(seq_lens), _ptr(block_refs), _ptr(status), ws, ws_bytes, _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_fork_kv_seqs")
+
+
+def bana_release_kv_blocks(block_table, keep_lens, block_refs, status, stream=None) -> None:
+    """The blocks behind the first ``keep_lens[b]`` tokens of every sequence given back; see include/bana_tokens.h."""
+    st = _calls().release(block_table, keep_lens, block_refs, status, stream)
+    if st is None:
+        B, mb, nb = _check_blocks(block_table, block_refs, status)
+        _need(keep_lens, "keep_lens", torch.int32, (B,))
+        _same_device(block_table, keep_lens, block_refs, status)
+        dims = bana_dims(B, 1, 1, HEAD_DIM, BLOCK_SIZE, mb, nb)
+        st = lib().bana_release_kv_blocks(ctypes.byref(dims), _ptr(block_table), _ptr(keep_lens), _ptr(block_refs),
+                                          _ptr(status), _stream(stream))
+    if st != BANA_OK:
+        raise BanaError(st, "bana_release_kv_blocks")

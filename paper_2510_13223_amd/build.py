@@ -22,8 +22,8 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libbana.so")
 SOURCES = ["attn_partial.hip", "merge.hip", "migrate.hip", "validate.hip", "debug_rows.hip", "gather_read.hip",
-           "scratch.hip",
-           "bana_api.cpp"]
+           "scratch.hip", "rows_attn.hip", "tokens.hip", "blocks.hip",
+           "bana_api.cpp", "tokens_api.cpp"]
 
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")

@@ -13,6 +13,7 @@
 #include <cmath>
 #include <string>
 
+#include "api_checks.h"
 #include "kernels.h"
 
 namespace {
@@ -73,7 +74,13 @@ constexpr int kMaxSideCopyGroups = 32;
 constexpr int64_t kMaxRows = int64_t{1} << 26;  // batch x num_q_heads: 64 threads per row stay below 2^32
 constexpr int64_t kMaxLaunchItems = UINT32_MAX;  // work-items of one launch (grid x workgroup size)
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+using bana::aligned16;
+using bana::check_dims;
+using bana::device_status;
+
+}  // namespace
+
+namespace bana {
 
 bana_status check_dims(const bana_dims* d) {
   if (d == nullptr) return BANA_ERR_INVALID;
@@ -97,6 +104,16 @@ bana_status check_dims(const bana_dims* d) {
     return BANA_ERR_UNSUPPORTED;
   return BANA_OK;
 }
+
+bana_status device_status(hipError_t e) {
+  if (e == hipSuccess) return BANA_OK;
+  g_last_error = hipGetErrorString(e);
+  return BANA_ERR_DEVICE;
+}
+
+}  // namespace bana
+
+namespace {
 
 struct Plan {
   int waves;      // wavefronts per workgroup
@@ -405,12 +422,6 @@ Plan make_plan(const bana_dims* d, Room room = Room::kAny) {
   p.nc = split ? std::max(1, std::min(p.nc, kMaxChunks)) : 1;
   if (((int64_t)p.nc * pairs + kMaxSideCopyGroups) * 64 * p.waves > kMaxLaunchItems) p.nc = 1;
   return p;
-}
-
-bana_status device_status(hipError_t e) {
-  if (e == hipSuccess) return BANA_OK;
-  g_last_error = hipGetErrorString(e);
-  return BANA_ERR_DEVICE;
 }
 
 }  // namespace

@@ -15,7 +15,7 @@
 #include <cstring>
 #include <initializer_list>
 
-#include "bana.h"
+#include "bana_tokens.h"
 
 namespace {
 
@@ -27,6 +27,13 @@ struct Api {
   decltype(&bana_decode_attn_heads) heads;
   decltype(&bana_merge_partials) merge;
   decltype(&bana_migrate_kv_blocks) migrate;
+  decltype(&bana_tree_attn) tree;
+  decltype(&bana_window_attn) window;
+  decltype(&bana_append_kv) append;
+  decltype(&bana_compact_kv_tokens) compact;
+  decltype(&bana_reserve_kv_blocks) reserve;
+  decltype(&bana_fork_kv_seqs) fork;
+  decltype(&bana_release_kv_blocks) release;
 };
 Api g_api{};
 PyObject* g_raw_stream = nullptr;  // torch._C._cuda_getCurrentRawStream
@@ -331,6 +338,240 @@ PyObject* migrate(PyObject*, PyObject* const* o, Py_ssize_t n) {
   });
 }
 
+// The cache of the calls on new tokens and blocks: pools [num_blocks][Hkv] and the block table.
+struct Cache {
+  const at::Tensor *k, *v, *table;
+  bana_dims dims{};
+
+  bool take_table(Args& a, PyObject* o) {
+    table = a.get(o, at::kInt);
+    if (table == nullptr || table->dim() != 2) return false;
+    dims.batch = (int32_t)table->size(0);
+    dims.max_blocks_per_seq = (int32_t)table->size(1);
+    dims.head_dim = 128;
+    dims.block_size = 16;
+    dims.num_q_heads = dims.num_kv_heads = 1;
+    return true;
+  }
+  bool take(Args& a, PyObject* ko, PyObject* vo, PyObject* to) {
+    if (!take_table(a, to)) return false;
+    k = a.get(ko, at::kBFloat16);
+    if (k == nullptr || k->dim() != 5) return false;
+    const int64_t nb = k->size(0), H = k->size(1);
+    if (k->sizes() != at::IntArrayRef({nb, H, 16, 16, 8})) return false;
+    v = a.get(vo, at::kBFloat16, {nb, H, 128, 16});
+    dims.num_q_heads = dims.num_kv_heads = (int32_t)H;
+    dims.num_blocks = nb;
+    return v != nullptr;
+  }
+};
+
+// What both attention calls on packed rows share.
+struct RowsAttention {
+  Cache c;
+  const at::Tensor *q, *row_begin, *out, *lse = nullptr, *workspace = nullptr;
+  int64_t rows;
+  int32_t out_type;
+  size_t workspace_bytes = 0;
+  float scale;
+
+  bool take(Args& a, PyObject* qo, PyObject* rb, PyObject* ko, PyObject* vo, PyObject* to, PyObject* oo, PyObject* lo,
+            PyObject* so, PyObject* wo, PyObject* py_dims) {
+    q = a.get(qo, at::kBFloat16);
+    if (q == nullptr || q->dim() != 3 || q->size(2) != 128 || !c.take(a, ko, vo, to)) return false;
+    rows = q->size(0);
+    const int64_t Hq = q->size(1);
+    c.dims.num_q_heads = (int32_t)Hq;
+    row_begin = a.get(rb, at::kInt, {(int64_t)c.dims.batch + 1});
+    out = a.any(oo);
+    if (row_begin == nullptr || out == nullptr || out->sizes() != q->sizes() || rows == 0) return false;
+    if (out->scalar_type() != at::kFloat && out->scalar_type() != at::kBFloat16) return false;
+    out_type = out->scalar_type() == at::kFloat ? BANA_OUT_F32 : BANA_OUT_BF16;
+    if (lo != Py_None && (lse = a.get(lo, at::kFloat, {rows, Hq})) == nullptr) return false;
+    if (!PyFloat_CheckExact(so)) return false;
+    scale = (float)PyFloat_AS_DOUBLE(so);
+    if (wo != Py_None) {
+      if ((workspace = a.any(wo)) == nullptr) return false;
+      workspace_bytes = (size_t)workspace->numel() * workspace->element_size();
+    }
+    if (py_dims == Py_None) return true;
+    if (Py_TYPE(py_dims) != reinterpret_cast<PyTypeObject*>(g_dims_type)) return false;
+    Py_buffer view;
+    if (PyObject_GetBuffer(py_dims, &view, PyBUF_SIMPLE) != 0) return false;
+    bana_dims d{};
+    const bool whole = view.len == (Py_ssize_t)sizeof(bana_dims);
+    if (whole) d = *static_cast<const bana_dims*>(view.buf);
+    PyBuffer_Release(&view);
+    const bana_dims& w = c.dims;
+    if (!whole || d.batch != w.batch || d.num_q_heads != w.num_q_heads || d.num_kv_heads != w.num_kv_heads ||
+        d.head_dim != w.head_dim || d.max_blocks_per_seq != w.max_blocks_per_seq || d.num_blocks != w.num_blocks)
+      return false;
+    c.dims = d;
+    return true;
+  }
+};
+
+// tree(q, row_begin, k, v, table, begin, end, tree_begin, mask, out, lse, scale, workspace, stream, dims)
+PyObject* tree(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    RowsAttention t;
+    void* s;
+    if (n != 15 || !t.take(a, o[0], o[1], o[2], o[3], o[4], o[9], o[10], o[11], o[12], o[14])) return kLook;
+    const int64_t B = t.c.dims.batch;
+    const at::Tensor* begin = a.get(o[5], at::kInt);
+    if (begin == nullptr || begin->dim() != 2 || begin->size(1) != B) return kLook;
+    const int64_t parts = begin->size(0);
+    const at::Tensor *end = a.get(o[6], at::kInt, {parts, B}), *at = a.get(o[7], at::kInt, {B});
+    const at::Tensor* mask = a.get(o[8], at::kLong, {t.rows});
+    if (!end || !at || !mask || !a.on_current_device() || !stream_handle(o[13], a.device, &s)) return kLook;
+    return WITHOUT_GIL(g_api.tree(&t.c.dims, t.rows, data<int32_t>(t.row_begin), data<void>(t.q), data<void>(t.c.k),
+                                  data<void>(t.c.v), data<int32_t>(t.c.table), data<int32_t>(begin),
+                                  data<int32_t>(end), (int32_t)parts, data<int32_t>(at), data<uint64_t>(mask), t.scale,
+                                  data<void>(t.out), t.out_type, data<float>(t.lse), data<void>(t.workspace),
+                                  t.workspace_bytes, s));
+  });
+}
+
+// window(q, row_begin, k, v, table, lens, window, sinks, out, lse, scale, begin, end, workspace, stream, dims)
+PyObject* window(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    RowsAttention t;
+    long long width, sinks;
+    void* s;
+    if (n != 16 || !int_arg(o[6], &width) || !int_arg(o[7], &sinks) || width != (int32_t)width ||
+        sinks != (int32_t)sinks || width < 1 || sinks < 0 ||
+        !t.take(a, o[0], o[1], o[2], o[3], o[4], o[8], o[9], o[10], o[13], o[15]))
+      return kLook;
+    const int64_t B = t.c.dims.batch;
+    const at::Tensor *lens = a.get(o[5], at::kInt, {B}), *begin = nullptr, *end = nullptr;
+    if ((o[11] == Py_None) != (o[12] == Py_None)) return kLook;
+    if (o[11] != Py_None) {
+      begin = a.get(o[11], at::kInt, {B});
+      end = a.get(o[12], at::kInt, {B});
+      if (!begin || !end) return kLook;
+    }
+    if (!lens || !a.on_current_device() || !stream_handle(o[14], a.device, &s)) return kLook;
+    return WITHOUT_GIL(g_api.window(&t.c.dims, t.rows, data<int32_t>(t.row_begin), data<void>(t.q), data<void>(t.c.k),
+                                    data<void>(t.c.v), data<int32_t>(t.c.table), data<int32_t>(lens),
+                                    data<int32_t>(begin), data<int32_t>(end), (int32_t)width, (int32_t)sinks, t.scale,
+                                    data<void>(t.out), t.out_type, data<float>(t.lse), data<void>(t.workspace),
+                                    t.workspace_bytes, s));
+  });
+}
+
+// append(k_rows, v_rows, row_begin, first_token, table, k, v, stream)
+PyObject* append(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    Cache c;
+    void* s;
+    if (n != 8 || !c.take(a, o[5], o[6], o[4])) return kLook;
+    const int64_t B = c.dims.batch, H = c.dims.num_kv_heads;
+    const at::Tensor* kr = a.get(o[0], at::kBFloat16);
+    if (kr == nullptr || kr->dim() != 3 || kr->size(0) == 0) return kLook;
+    const int64_t rows = kr->size(0);
+    const at::Tensor* vr = a.get(o[1], at::kBFloat16, {rows, H, 128});
+    const at::Tensor *rb = a.get(o[2], at::kInt, {B + 1}), *first = a.get(o[3], at::kInt, {B});
+    if (!vr || kr->sizes() != vr->sizes() || !rb || !first || !a.on_current_device() ||
+        !stream_handle(o[7], a.device, &s))
+      return kLook;
+    return WITHOUT_GIL(g_api.append(&c.dims, rows, data<int32_t>(rb), data<int32_t>(first), data<void>(kr),
+                                    data<void>(vr), data<int32_t>(c.table), data<void>(c.k), data<void>(c.v), s));
+  });
+}
+
+// compact(k, v, table, first_token, kept, n_kept, stream)
+PyObject* compact(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    Cache c;
+    void* s;
+    if (n != 7 || !c.take(a, o[0], o[1], o[2])) return kLook;
+    const int64_t B = c.dims.batch;
+    const at::Tensor *first = a.get(o[3], at::kInt, {B}), *kept = a.get(o[4], at::kInt);
+    const at::Tensor* count = a.get(o[5], at::kInt, {B});
+    if (!first || !kept || kept->dim() != 2 || kept->size(0) != B || kept->size(1) == 0 ||
+        kept->size(1) > INT32_MAX || !count || !a.on_current_device() || !stream_handle(o[6], a.device, &s))
+      return kLook;
+    return WITHOUT_GIL(g_api.compact(&c.dims, data<void>(c.k), data<void>(c.v), data<int32_t>(c.table),
+                                     data<int32_t>(first), data<int32_t>(kept), (int32_t)kept->size(1),
+                                     data<int32_t>(count), s));
+  });
+}
+
+// The counts of a call on blocks, its status word and workspace.
+struct Blocks {
+  const at::Tensor *refs, *status, *workspace = nullptr;
+  size_t workspace_bytes = 0;
+
+  bool take(Args& a, Cache& c, PyObject* ro, PyObject* so, PyObject* wo) {
+    refs = a.get(ro, at::kInt);
+    status = a.get(so, at::kInt, {1});
+    if (refs == nullptr || refs->dim() != 1 || status == nullptr) return false;
+    c.dims.num_blocks = refs->size(0);
+    if (wo == nullptr) return true;
+    workspace = a.any(wo);
+    if (workspace == nullptr) return false;
+    workspace_bytes = (size_t)workspace->numel() * workspace->element_size();
+    return true;
+  }
+};
+
+// reserve(table, lens, need, refs, status, workspace, stream)
+PyObject* reserve(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    Cache c;
+    Blocks x;
+    void* s;
+    if (n != 7 || !c.take_table(a, o[0]) || !x.take(a, c, o[3], o[4], o[5])) return kLook;
+    const int64_t B = c.dims.batch;
+    const at::Tensor *lens = a.get(o[1], at::kInt, {B}), *need = a.get(o[2], at::kInt, {B});
+    if (!lens || !need || !a.on_current_device() || !stream_handle(o[6], a.device, &s)) return kLook;
+    return WITHOUT_GIL(g_api.reserve(&c.dims, data<int32_t>(c.table), data<int32_t>(lens), data<int32_t>(need),
+                                     data<int32_t>(x.refs), data<int32_t>(x.status), data<void>(x.workspace),
+                                     x.workspace_bytes, s));
+  });
+}
+
+// fork(src, dst, k, v, table, lens, refs, status, workspace, stream)
+PyObject* fork(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    Cache c;
+    Blocks x;
+    void* s;
+    if (n != 10 || !c.take(a, o[2], o[3], o[4])) return kLook;
+    const int64_t B = c.dims.batch, nb = c.dims.num_blocks;
+    const at::Tensor *lens = a.get(o[5], at::kInt, {B}), *src = a.get(o[0], at::kInt);
+    if (!x.take(a, c, o[6], o[7], o[8]) || c.dims.num_blocks != nb) return kLook;
+    if (!lens || !src || src->dim() != 1 || src->size(0) == 0 || src->size(0) > B) return kLook;
+    const at::Tensor* dst = a.get(o[1], at::kInt, {src->size(0)});
+    if (!dst || !a.on_current_device() || !stream_handle(o[9], a.device, &s)) return kLook;
+    return WITHOUT_GIL(g_api.fork(&c.dims, data<int32_t>(src), data<int32_t>(dst), (int32_t)src->size(0),
+                                  data<void>(c.k), data<void>(c.v), data<int32_t>(c.table), data<int32_t>(lens),
+                                  data<int32_t>(x.refs), data<int32_t>(x.status), data<void>(x.workspace),
+                                  x.workspace_bytes, s));
+  });
+}
+
+// release(table, keep, refs, status, stream)
+PyObject* release(PyObject*, PyObject* const* o, Py_ssize_t n) {
+  return guarded([&]() -> long {
+    Args a;
+    Cache c;
+    Blocks x;
+    void* s;
+    if (n != 5 || !c.take_table(a, o[0]) || !x.take(a, c, o[2], o[3], nullptr)) return kLook;
+    const at::Tensor* keep = a.get(o[1], at::kInt, {(int64_t)c.dims.batch});
+    if (!keep || !a.on_current_device() || !stream_handle(o[4], a.device, &s)) return kLook;
+    return WITHOUT_GIL(g_api.release(&c.dims, data<int32_t>(c.table), data<int32_t>(keep), data<int32_t>(x.refs),
+                                     data<int32_t>(x.status), s));
+  });
+}
+
 // setup((address of each C ABI call, in Api's order), raw-stream function, stream type, bana_dims type)
 PyObject* setup(PyObject*, PyObject* const* o, Py_ssize_t n) {
   constexpr Py_ssize_t kCalls = sizeof(Api) / sizeof(void*);
@@ -353,7 +594,8 @@ PyObject* setup(PyObject*, PyObject* const* o, Py_ssize_t n) {
 
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(f)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {METHOD(setup), METHOD(partial), METHOD(noalloc), METHOD(fused), METHOD(heads),
-                           METHOD(merge), METHOD(migrate), {nullptr, nullptr, 0, nullptr}};
+                           METHOD(merge), METHOD(migrate), METHOD(tree), METHOD(window), METHOD(append),
+                           METHOD(compact), METHOD(reserve), METHOD(fork), METHOD(release), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

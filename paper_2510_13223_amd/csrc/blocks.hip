@@ -1,0 +1,248 @@
+// blocks.hip -- blocks of the cache handed out, shared and taken back on the device (gfx950).
+//
+// The state is the block table and one count per block; a block with the count 0 is free, and the lowest
+// free numbers are taken first, so there is no free list whose order could depend on timing.  A call
+// that takes blocks first makes its plan in one workgroup (what is asked for, whether it can be had, which
+// blocks), then carries it out; a plan that cannot be carried out changes nothing but *status.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "paged_addr.h"
+#include "tokens.h"
+
+namespace bana {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kPlanThreads = 1024;
+constexpr int kPlanWaves = kPlanThreads / 64;
+
+__device__ __forceinline__ int blocks_of(int64_t tokens) {
+  return tokens <= 0 ? 0 : (int)((tokens + kBlockSize - 1) / kBlockSize);
+}
+
+// Exclusive prefix sum of x over the workgroup, and the sum of all; every thread calls it.
+__device__ __forceinline__ int block_scan(int x, int* sm, int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int incl = x;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int y = __shfl_up(incl, off);
+    if (lane >= off) incl += y;
+  }
+  __syncthreads();  // sm may still be read from the scan before
+  race_check_delay(wave);
+  if (lane == 63) sm[wave] = incl;
+  __syncthreads();
+  race_check_barrier();
+  int before = incl - x, all = 0;
+#pragma unroll
+  for (int w = 0; w < kPlanWaves; ++w) {
+    if (w < wave) before += sm[w];
+    all += sm[w];
+  }
+  *total = all;
+  return before;
+}
+
+// The numbers of the `need` lowest free blocks into list[0..need); the number found (>= need unless there
+// are fewer).
+__device__ __forceinline__ int64_t find_free(const int32_t* __restrict__ refs, int64_t num_blocks, int64_t need,
+                                             int32_t* __restrict__ list, int* sm) {
+  int64_t found = 0;
+  for (int64_t base = 0; base < num_blocks && found < need; base += kPlanThreads) {
+    const int64_t blk = base + threadIdx.x;
+    const bool is_free = blk < num_blocks && refs[blk] == 0;
+    int total;
+    const int at = block_scan(is_free, sm, &total);
+    if (is_free && found + at < need) list[found + at] = (int32_t)blk;
+    found += total;
+  }
+  return found;
+}
+
+// Workspace: [0] 1 if the plan holds, [2..] 64-bit need; [64, 64 + B) counts or marks, [64 + B, 64 + 2 B) prefix
+// sums, then the list of blocks.
+__global__ __launch_bounds__(kPlanThreads) void reserve_kernel(int32_t* __restrict__ table,
+                                                               const int32_t* __restrict__ lens,
+                                                               const int32_t* __restrict__ need,
+                                                               int32_t* __restrict__ refs, int64_t num_blocks,
+                                                               int32_t* __restrict__ status,
+                                                               int32_t* __restrict__ ws, CacheShape s) {
+  __shared__ int sm[kPlanWaves];
+  int32_t* before = ws + 64;
+  int32_t* list = ws + 64 + 2 * (int64_t)s.B;
+  int64_t total = 0;
+  bool wide = false;
+  for (int b0 = 0; b0 < s.B; b0 += kPlanThreads) {
+    const int b = b0 + threadIdx.x;
+    int count = 0;
+    if (b < s.B) {
+      const int j1 = blocks_of(need[b]);
+      wide |= j1 > s.max_blocks;
+      for (int j = blocks_of(lens[b]); j < min(j1, s.max_blocks); ++j)
+        count += table[(int64_t)b * s.max_blocks + j] < 0;
+    }
+    int sum;
+    const int at = block_scan(count, sm, &sum);
+    if (b < s.B) before[b] = (int32_t)(total + at);
+    total += sum;
+  }
+  const bool too_wide = __syncthreads_or(wide);
+  const int64_t found = too_wide || total > num_blocks ? 0 : find_free(refs, num_blocks, total, list, sm);
+  if (too_wide || found < total) {
+    if (threadIdx.x == 0) atomicMax(status, too_wide ? 3 : 1);
+    return;
+  }
+  __syncthreads();
+  for (int b = threadIdx.x; b < s.B; b += kPlanThreads) {
+    int at = before[b];
+    for (int j = blocks_of(lens[b]); j < blocks_of(need[b]); ++j) {
+      int32_t* entry = table + (int64_t)b * s.max_blocks + j;
+      if (*entry >= 0) continue;
+      const int32_t blk = list[at++];
+      *entry = blk;
+      refs[blk] = 1;
+    }
+  }
+}
+
+__device__ __forceinline__ int64_t length_of(const int32_t* __restrict__ lens, int b, const CacheShape& s) {
+  return min((int64_t)max(lens[b], 0), (int64_t)s.max_blocks * kBlockSize);
+}
+
+__global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const int32_t* __restrict__ src,
+                                                                 const int32_t* __restrict__ dst, int n,
+                                                                 const int32_t* __restrict__ table,
+                                                                 const int32_t* __restrict__ lens,
+                                                                 int32_t* __restrict__ refs, int64_t num_blocks,
+                                                                 int32_t* __restrict__ status,
+                                                                 int32_t* __restrict__ ws, CacheShape s) {
+  __shared__ int sm[kPlanWaves];
+  int32_t* mark = ws + 64;            // [B]: 1 + the fork that writes the sequence, 0: none
+  int32_t* list = ws + 64 + s.B;      // [min(n, B)] block of each fork that takes one, in order
+  for (int b = threadIdx.x; b < s.B; b += kPlanThreads) mark[b] = 0;
+  __syncthreads();
+  bool bad = n > s.B;
+  for (int i = threadIdx.x; i < n && !bad; i += kPlanThreads) {
+    const int d = dst[i], c = src[i];
+    bad = d < 0 || d >= s.B || c < 0 || c >= s.B || table[(int64_t)d * s.max_blocks] != -1 ||
+          atomicExch(mark + d, 1) != 0;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n && !bad; i += kPlanThreads)
+    bad = __hip_atomic_load(mark + src[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
+  if (__syncthreads_or(bad)) {
+    if (threadIdx.x == 0) {
+      atomicMax(status, 2);
+      ws[0] = 0;
+    }
+    return;
+  }
+  int64_t total = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int sum;
+    const int at = block_scan(i < n && length_of(lens, src[i], s) % kBlockSize != 0, sm, &sum);
+    if (i < n) mark[i] = (int32_t)(total + at);  // place in the list (the marks are done with)
+    total += sum;
+  }
+  const int64_t found = total > num_blocks ? 0 : find_free(refs, num_blocks, total, list, sm);
+  if (found < total) {
+    if (threadIdx.x == 0) {
+      atomicMax(status, 1);
+      ws[0] = 0;
+    }
+    return;
+  }
+  __syncthreads();
+  for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) refs[list[i]] = 1;
+  if (threadIdx.x == 0) ws[0] = 1;
+}
+
+// One workgroup per fork: the shared entries, and the copy of the last block if it is partly filled.
+__global__ __launch_bounds__(256) void fork_kernel(const int32_t* __restrict__ src, const int32_t* __restrict__ dst,
+                                                   u32x4* __restrict__ k, u32x4* __restrict__ v,
+                                                   int32_t* __restrict__ table, int32_t* __restrict__ lens,
+                                                   int32_t* __restrict__ refs, int32_t* __restrict__ status,
+                                                   const int32_t* __restrict__ ws, CacheShape s) {
+  if (ws[0] == 0) return;
+  const int i = blockIdx.x;
+  const int from = src[i], to = dst[i];
+  const int64_t len = length_of(lens, from, s);
+  const int whole = (int)(len / kBlockSize);
+  const int32_t* of = table + (int64_t)from * s.max_blocks;
+  int32_t* entry = table + (int64_t)to * s.max_blocks;
+  bool bad = false;
+  for (int j = threadIdx.x; j < whole; j += 256) {
+    const int32_t blk = of[j];
+    entry[j] = blk;
+    if (blk >= 0 && blk <= s.last_block) atomicAdd(refs + blk, 1);
+    else bad = true;
+  }
+  if (len % kBlockSize != 0) {
+    const int32_t fresh = ws[64 + s.B + ws[64 + i]];
+    const int32_t blk = of[whole];
+    if (threadIdx.x == 0) entry[whole] = fresh;
+    if (blk >= 0 && blk <= s.last_block) {
+      const int64_t n16 = (int64_t)s.Hkv * kTileElems / 8;
+      for (int64_t x = threadIdx.x; x < n16; x += 256) {
+        k[fresh * n16 + x] = k[blk * n16 + x];
+        v[fresh * n16 + x] = v[blk * n16 + x];
+      }
+    } else {
+      bad = true;
+    }
+  }
+  if (bad) atomicMax(status, 4);
+  if (threadIdx.x == 0) lens[to] = (int32_t)len;
+}
+
+__global__ __launch_bounds__(256) void release_kernel(int32_t* __restrict__ table, const int32_t* __restrict__ keep,
+                                                      int32_t* __restrict__ refs, int32_t* __restrict__ status,
+                                                      CacheShape s) {
+  for (int b = blockIdx.x; b < s.B; b += gridDim.x) {
+    for (int64_t j = (int64_t)blocks_of(keep[b]) + threadIdx.x; j < s.max_blocks; j += 256) {
+      int32_t* entry = table + (int64_t)b * s.max_blocks + j;
+      const int32_t blk = *entry;
+      if (blk == -1) continue;
+      *entry = -1;
+      if (blk < 0 || blk > s.last_block) {
+        atomicMax(status, 4);
+      } else if (atomicSub(refs + blk, 1) <= 0) {
+        atomicAdd(refs + blk, 1);
+        atomicMax(status, 4);
+      }
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_reserve(int32_t* table, const int32_t* lens, const int32_t* need, int32_t* refs, int64_t num_blocks,
+                          int32_t* status, int32_t* workspace, CacheShape s, hipStream_t stream) {
+  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kPlanThreads), 0, stream, table, lens, need, refs, num_blocks,
+                     status, workspace, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_fork(const int32_t* src, const int32_t* dst, int n, void* k, void* v, int32_t* table, int32_t* lens,
+                       int32_t* refs, int64_t num_blocks, int32_t* status, int32_t* workspace, CacheShape s,
+                       hipStream_t stream) {
+  hipLaunchKernelGGL(fork_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, src, dst, n, table, lens, refs,
+                     num_blocks, status, workspace, s);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(fork_kernel, dim3((unsigned)n), dim3(256), 0, stream, src, dst, static_cast<u32x4*>(k),
+                     static_cast<u32x4*>(v), table, lens, refs, status, workspace, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_release(int32_t* table, const int32_t* keep, int32_t* refs, int32_t* status, CacheShape s,
+                          hipStream_t stream) {
+  hipLaunchKernelGGL(release_kernel, dim3((unsigned)(s.B < 65536 ? s.B : 65536)), dim3(256), 0, stream, table, keep, refs, status, s);
+  return hipGetLastError();
+}
+
+}  // namespace bana

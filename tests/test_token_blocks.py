@@ -1,0 +1,326 @@
+"""New tokens into the cache, kept tokens moved together, blocks handed out, shared and taken back: every value and
+number against the plain forms; a draft step and forked sequences with all of them together."""
+
+import math
+import random
+
+import pytest
+import torch
+
+import token_cases as tc
+from paper_2510_13223_amd import bana
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def same(x, y):
+    """Equal bit for bit (pools hold NaN)."""
+    x, y = x.cpu(), y.cpu()
+    if x.dtype == torch.bfloat16:
+        x, y = x.view(torch.int16), y.view(torch.int16)
+    return torch.equal(x, y)
+
+
+@pytest.mark.parametrize("hkv,lens,news", [
+    (1, [0], [1]), (8, [15, 16, 17], [1, 1, 1]), (2, [0, 100, 5], [33, 0, 64]), (3, [7], [300]),
+    (4, [2] * 70, [1] * 70), (40, [1, 30], [20, 3]), (5, [0, 0, 31], [0, 0, 2]), (8, [3, 900], [513, 1000]),
+])
+def test_append(hkv, lens, news):
+    rb, rows = tc.rows_of(news, pad=3, first=2)
+    cache = tc.Cache([a + n for a, n in zip(lens, news)], hkv, 3)
+    g = torch.Generator().manual_seed(4)
+    kr, vr = (torch.randn((rows, hkv, tc.D), generator=g).to(torch.bfloat16) for _ in range(2))
+    k, v, table = cache.k.to(DEV), cache.v.to(DEV), cache.table.to(DEV)
+    tc.append(kr, vr, rb, lens, cache.table, cache.k, cache.v)
+    bana.bana_append_kv(kr.to(DEV), vr.to(DEV), ints(rb), ints(lens), table, k, v)
+    assert same(k, cache.k) and same(v, cache.v)
+
+
+def test_append_skips_tokens_without_a_block():
+    cache = tc.Cache([40, 33], 2, 5)
+    cache.table[0, 1], cache.table[1, 2] = -1, cache.num_blocks + 7
+    rb, rows = tc.rows_of([30, 20, ])
+    kr = torch.randn((rows, 2, tc.D)).to(torch.bfloat16)
+    k, v = cache.k.to(DEV), cache.v.to(DEV)
+    first = [-3, 25]  # before the table and past its end
+    tc.append(kr, kr, rb, first, cache.table, cache.k, cache.v)
+    bana.bana_append_kv(kr.to(DEV), kr.to(DEV), ints(rb), ints(first), cache.table.to(DEV), k, v)
+    assert same(k, cache.k) and same(v, cache.v)
+
+
+@pytest.mark.parametrize("hkv,lens,first,keep", [
+    (1, [20], [0], 0.5), (8, [100, 33], [40, 17], 0.3), (2, [500, 0, 31], [0, 0, 15], 0.9), (3, [77] * 5, [13] * 5, 0.1),
+    (40, [64], [0], 1.0), (2, [64, 64], [1, 30], 0.0), (4, [3000, 1], [5, 0], 0.6),
+])
+def test_compact(hkv, lens, first, keep):
+    rng = random.Random(7)
+    cache = tc.Cache(lens, hkv, 6)
+    kept = [sorted(rng.sample(range(n - f), int(round(keep * (n - f))))) for n, f in zip(lens, first)]
+    most = max(1, max(map(len, kept)) + 2)
+    counts = [len(x) for x in kept]
+    padded = torch.tensor([x + [2 ** 31 - 1] * (most - len(x)) for x in kept], dtype=torch.int32)
+    k, v = cache.k.to(DEV), cache.v.to(DEV)
+    tc.compact(cache.k, cache.v, cache.table, first, padded, counts)
+    bana.bana_compact_kv_tokens(k, v, cache.table.to(DEV), ints(first), padded.to(DEV), ints(counts))
+    assert same(k, cache.k) and same(v, cache.v)
+
+
+def test_compact_stays_inside_whatever_the_numbers():
+    """Counts past the list, places past the table, entries of no block: skipped."""
+    cache = tc.Cache([60, 40], 2, 8, width=5)
+    cache.table[0, 2] = -1
+    kept = torch.tensor([[0, 3, 35, 50, 70, 10 ** 9], [1, 2, 3, 4, 5, 6]], dtype=torch.int32)
+    k, v = cache.k.to(DEV), cache.v.to(DEV)
+    tc.compact(cache.k, cache.v, cache.table, [4, 37], kept, [9, -1])
+    bana.bana_compact_kv_tokens(k, v, cache.table.to(DEV), ints([4, 37]), kept.to(DEV), ints([9, -1]))
+    assert same(k, cache.k) and same(v, cache.v)
+
+
+class Pool:
+    """A table with its counts, on both sides."""
+
+    def __init__(self, lens, num_blocks, width, seed, hkv=2):
+        g = torch.Generator().manual_seed(seed)
+        perm = torch.randperm(num_blocks, generator=g).tolist()
+        self.table = torch.full((len(lens), width), -1, dtype=torch.int32)
+        self.refs = torch.zeros(num_blocks, dtype=torch.int32)
+        for b, n in enumerate(lens):
+            for j in range(tc.blocks_of(n)):
+                self.table[b, j] = perm.pop()
+                self.refs[self.table[b, j]] += 1
+        self.lens = torch.tensor(lens, dtype=torch.int32)
+        self.status = torch.zeros(1, dtype=torch.int32)
+        self.k = torch.randn((num_blocks, hkv, 16, 16, 8), generator=g).to(torch.bfloat16)
+        self.v = torch.randn((num_blocks, hkv, 128, 16), generator=g).to(torch.bfloat16)
+        self.upload()
+
+    NAMES = ("table", "refs", "lens", "status", "k", "v")
+
+    def upload(self):
+        self.dev = {n: getattr(self, n).to(DEV) for n in self.NAMES}
+        n = bana.bana_kv_blocks_workspace_bytes(*self.table.shape, len(self.refs))
+        self.ws = torch.full((n,), 0x7F, dtype=torch.uint8, device=DEV)
+
+    def reserve(self, need):
+        d = self.dev
+        tc.reserve(self.table, self.lens, need, self.refs, self.status)
+        bana.bana_reserve_kv_blocks(d["table"], d["lens"], ints(need), d["refs"], d["status"], self.ws)
+
+    def release(self, keep):
+        d = self.dev
+        tc.release(self.table, keep, self.refs, self.status)
+        bana.bana_release_kv_blocks(d["table"], ints(keep), d["refs"], d["status"])
+
+    def fork(self, src, dst):
+        d = self.dev
+        tc.fork(src, dst, self.k, self.v, self.table, self.lens, self.refs, self.status)
+        bana.bana_fork_kv_seqs(ints(src), ints(dst), d["k"], d["v"], d["table"], d["lens"], d["refs"], d["status"],
+                               self.ws)
+
+    def check(self, status=0):
+        for n in self.NAMES:
+            assert same(self.dev[n], getattr(self, n)), n
+        assert int(self.status) == status
+
+
+def test_reserve_and_release():
+    p = Pool([0, 1, 16, 17, 250, 0], 60, 24, 1)
+    p.reserve([0, 1, 17, 40, 384, 33])
+    p.check()
+    p.reserve([0, 1, 17, 40, 384, 33])  # what is there stays
+    p.check()
+    p.release([-5, 0, 16, 33, 100, 10 ** 9])
+    p.check()
+    p.reserve([5, 100, 16, 0, 3, 2])
+    p.check()
+    p.release([0] * 6)
+    p.check()
+    assert int(p.refs.sum()) == 0
+
+
+@pytest.mark.parametrize("batch,blocks,width", [(3, 5000, 400), (2500, 20000, 9), (70, 70000, 30)])
+def test_reserve_in_large_pools(batch, blocks, width):
+    """Free blocks far apart, more sequences than threads of the plan, all of the pool taken."""
+    rng = random.Random(batch)
+    p = Pool([rng.randint(0, width * 4) for _ in range(batch)], blocks, width, 2)
+    taken = torch.randperm(blocks)[:blocks // 2]
+    p.refs[taken] += 1  # blocks that others hold
+    p.upload()
+    p.reserve([rng.randint(0, width * 8) for _ in range(batch)])
+    p.check()
+    p.release([rng.randint(0, width * 8) for _ in range(batch)])
+    p.check()
+
+
+def test_all_blocks_and_one_too_many():
+    p = Pool([0, 0], 7, 8, 3)
+    p.reserve([4 * 16, 3 * 16 + 1])  # eight of seven
+    p.check(1)
+    p.status.zero_()
+    p.upload()
+    p.reserve([4 * 16, 3 * 16])
+    p.check()
+    assert int(p.refs.sum()) == 7
+    p.reserve([8 * 16 + 1, 3 * 16])  # wider than the table
+    p.check(3)
+    p.reserve([5 * 16, 3 * 16])  # nothing free; the higher code stays
+    p.check(3)
+
+
+def test_release_reports_blocks_without_references():
+    p = Pool([40, 40], 9, 3, 4)
+    p.table[0, 1] = p.table[1, 2]  # a block with one count named twice
+    p.table[0, 2], p.table[1, 0] = 9, -7
+    p.upload()
+    p.release([0, 0])
+    p.check(4)
+
+
+def test_fork():
+    p = Pool([33, 16, 0, 100, 15] + [0] * 9, 40, 8, 5)
+    p.fork([0, 0, 1, 2, 3, 4, 3], [5, 13, 6, 7, 8, 9, 12])  # a source twice, an empty source, whole blocks only
+    p.check()
+    p.release([33, 16, 0, 40, 0] + [0] * 4 + [15] + [0] * 4)
+    p.check()
+    p.fork([9], [5])
+    p.check()
+
+
+def test_fork_refusals_change_nothing():
+    for src, dst in (([0, 1], [3, 3]), ([0], [1]), ([0, 3], [3, 4]), ([9], [3]), ([-1], [3]), ([0], [5]), ([2], [-1])):
+        p = Pool([33, 16, 0, 0, 0], 9, 4, 6)
+        p.fork(src, dst)
+        p.check(2)
+    p = Pool([33, 16, 20, 0, 0, 0, 0], 7, 4, 7)  # one block free, two wanted
+    p.fork([0, 1, 2], [3, 4, 5])
+    p.check(1)
+    p = Pool([33, 20, 0, 0], 9, 4, 8)
+    p.table[0, 0], p.table[1, 1] = -1, 99
+    p.upload()
+    p.fork([0, 1], [2, 3])
+    p.check(4)
+
+
+def test_many_forks():
+    """More forks than threads of the plan, one parent of many."""
+    n = 1500
+    p = Pool([40, 64, 7] + [0] * n, 4000, 5, 9, hkv=1)
+    rng = random.Random(10)
+    dst = list(range(3, 3 + n))
+    rng.shuffle(dst)
+    p.fork([rng.choice([0, 0, 1, 2]) for _ in range(n)], dst)
+    p.check()
+    p.release([40, 64, 7] + [0] * n)
+    p.check()
+
+
+def test_draft_steps_and_forks_together():
+    """Prompts, forks and speculative steps over one cache, as a server makes them, each attention against 64 bits and
+    the cache's tokens against a dense copy."""
+    rng = random.Random(11)
+    hq, hkv, B, width, blocks = 8, 2, 6, 12, 50
+    k = torch.full((blocks, hkv, 16, 16, 8), math.nan, dtype=torch.bfloat16, device=DEV)
+    v = torch.full((blocks, hkv, 128, 16), math.nan, dtype=torch.bfloat16, device=DEV)
+    table = torch.full((B, width), -1, dtype=torch.int32, device=DEV)
+    refs, status = torch.zeros(blocks, dtype=torch.int32, device=DEV), ints([0])
+    lens = torch.zeros(B, dtype=torch.int32, device=DEV)
+    ws = torch.empty(bana.bana_kv_blocks_workspace_bytes(B, width, blocks), dtype=torch.uint8, device=DEV)
+    g = torch.Generator().manual_seed(12)
+
+    class Dense:
+        pass
+
+    dense = Dense()
+    dense.hkv = hkv
+    dense.keys = [torch.zeros((0, hkv, tc.D), dtype=torch.bfloat16) for _ in range(B)]
+    dense.values = [torch.zeros((0, hkv, tc.D), dtype=torch.bfloat16) for _ in range(B)]
+
+    def step(news, attend):
+        """New tokens of each sequence into the cache and `attend` over them."""
+        rb, rows = tc.rows_of(news)
+        kr, vr = (torch.randn((rows, hkv, tc.D), generator=g).to(torch.bfloat16) for _ in range(2))
+        q = torch.randn((rows, hq, tc.D), generator=g).to(torch.bfloat16)
+        before = [len(x) for x in dense.keys]
+        for b in range(B):
+            dense.keys[b] = torch.cat([dense.keys[b], kr[rb[b]:rb[b + 1]]])
+            dense.values[b] = torch.cat([dense.values[b], vr[rb[b]:rb[b + 1]]])
+        need = ints([n + m for n, m in zip(before, news)])
+        bana.bana_reserve_kv_blocks(table, lens, need, refs, status, ws)
+        bana.bana_append_kv(kr.to(DEV), vr.to(DEV), ints(rb), lens, table, k, v)
+        out = torch.empty((rows, hq, tc.D), device=DEV)
+        lse = torch.empty((rows, hq), device=DEV)
+        sees = attend(q.to(DEV), ints(rb), rb, before, out, lse)
+        want = tc.attention(q, rb, dense, sees, 0.0884)
+        tc.check_attention(out.cpu(), lse.cpu(), want, False)
+        return need
+
+    def window(q, rbd, rb, before, out, lse):
+        total = ints([n + rb[b + 1] - rb[b] for b, n in enumerate(before)])
+        bana.bana_window_attn(q, rbd, k, v, table, total, 30, 2, out, lse, scale=0.0884)
+        return tc.window_sees(total.tolist(), [rb[b + 1] - rb[b] for b in range(B)], 30, 2)
+
+    lens = step([35, 48, 7, 0, 0, 0], window)
+    bana.bana_fork_kv_seqs(ints([0, 0, 2]), ints([3, 5, 4]), k, v, table, lens, refs, status, ws)
+    for b, s in ((3, 0), (5, 0), (4, 2)):
+        dense.keys[b], dense.values[b] = dense.keys[s].clone(), dense.values[s].clone()
+    assert lens.tolist() == [35, 48, 7, 35, 7, 35] and int(status) == 0
+    for _ in range(4):
+        news = [rng.choice([0, 1, 5, 12]) for _ in range(B)]
+        trees = [tc.random_tree(n, rng) for n in news]
+
+        def tree(q, rbd, rb, before, out, lse):
+            masks = [m for t in trees for m in t]
+            begin, end = [[0] * B], [before]
+            bana.bana_tree_attn(q, rbd, k, v, table, ints(begin), ints(end), lens, tc.signed(masks).to(DEV), out, lse,
+                                scale=0.0884)
+            return tc.tree_sees(begin, end, before, masks, rb)
+
+        if sum(news) == 0:
+            continue
+        step(news, tree)
+        # The longest path of each tree is accepted; the others' blocks go back.
+        paths = [[] if not t else [j for j in range(n) if max(t, key=lambda m: bin(m).count("1")) >> j & 1]
+                 for t, n in zip(trees, news)]
+        most = max(map(len, paths))
+        kept = torch.tensor([p + [0] * (most - len(p)) for p in paths], dtype=torch.int32, device=DEV)
+        bana.bana_compact_kv_tokens(k, v, table, lens, kept, ints([len(p) for p in paths]))
+        for b in range(B):
+            n = len(dense.keys[b]) - news[b]
+            at = list(range(n)) + [n + j for j in paths[b]]
+            dense.keys[b], dense.values[b] = dense.keys[b][at], dense.values[b][at]
+        lens = ints([len(x) for x in dense.keys])
+        bana.bana_release_kv_blocks(table, lens, refs, status)
+        for b in range(B):
+            for t in range(len(dense.keys[b])):
+                key, value = tc.get(k, v, int(table[b, t // 16]), t % 16)
+                assert same(key, dense.keys[b][t]) and same(value, dense.values[b][t]), (b, t)
+    named = torch.bincount(table[table >= 0].long(), minlength=blocks)
+    assert torch.equal(named.cpu().int(), refs.cpu()) and int(status) == 0
+    bana.bana_release_kv_blocks(table, ints([0] * B), refs, status)
+    assert int(refs.abs().sum()) == 0 and int(status) == 0
+
+
+def test_captured_block_calls_replay():
+    """A draft step's block calls in a graph: every replay leaves what an eager run leaves."""
+    p = Pool([20, 0, 47], 30, 8, 13)
+    d = p.dev
+    need = ints([60, 40, 90])
+    keep = d["lens"].clone()
+    before = {n: x.clone() for n, x in d.items()}
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        bana.bana_reserve_kv_blocks(d["table"], d["lens"], need, d["refs"], d["status"], p.ws)
+        bana.bana_release_kv_blocks(d["table"], keep, d["refs"], d["status"])
+        bana.bana_reserve_kv_blocks(d["table"], d["lens"], need, d["refs"], d["status"], p.ws)
+    tc.reserve(p.table, p.lens, need.tolist(), p.refs, p.status)
+    for _ in range(4):
+        for n in d:
+            d[n].copy_(before[n])
+        graph.replay()
+        torch.cuda.synchronize()
+        p.check()
