@@ -2,16 +2,16 @@
 //
 // Row r of sequence b, query head h, over the tokens that the row sees:
 //   s_t = scale q[r][h].k_t,  out = sum_t exp(s_t - lse) v_t,  lse = ln sum_t exp(s_t)
-// Two kinds of sight share one kernel:
+// Two kinds of sight share the kernels:
 //  * tree: some ranges of the context, whole, and the nodes whose bit is set in the row's mask;
 //  * window: tokens t <= pos with pos - t < window or t < sinks.
 //
 // The columns of the score product are the (row, head of the group) pairs of one sequence and kv head,
-// c = i G + h, 16 to a tile; one wavefront takes one tile and walks the blocks that any of its rows sees
-// with the products, layouts and one-pass softmax of the decode kernel (attn_partial.hip).  A tile's
-// number among all tiles of a kv head is floor(row_begin[b] G / 16) + b plus its place in the sequence:
-// unique, as a sequence of n rows has at most floor(end G / 16) - floor(begin G / 16) + 1 tiles, so the
-// grid follows from the number of rows and sequences alone and a wavefront finds its sequence by search.
+// c = i G + h.  A workgroup takes a tile of CT neighbouring columns of one sequence and kv head and walks
+// the blocks that any of its rows sees.  A tile's number among all tiles of a kv head is
+// floor(row_begin[b] G / CT) + b plus its place in the sequence: unique, as a sequence's columns [x, y)
+// make at most floor(y / CT) - floor(x / CT) + 1 tiles, so the grid follows from the number of rows and sequences
+// alone and a workgroup finds its sequence by search.
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -24,234 +24,568 @@ namespace bana {
 namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kCols = 16;
 constexpr int kDimTiles = kHeadDim / 16;
 constexpr float kLn2 = 0.6931471805599453f;
 
-__device__ __forceinline__ uint32_t bf16_bits(float x) {
-  const uint32_t u = __builtin_bit_cast(uint32_t, x);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (u >> 16) | 0x40u;  // NaN stays NaN
-  return (u + 0x7FFFu + ((u >> 16) & 1u)) >> 16;
-}
-__device__ __forceinline__ float bf16_value(uint32_t bits) { return __builtin_bit_cast(float, bits << 16); }
+__device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The token ranges that the rows of a tile see, one per lane, as a list of blocks (as in the decode kernel).
+// Two floats rounded to bf16 (nearest, ties to even), the first in the low half.
+__device__ __forceinline__ uint32_t bf16_pair(float x, float y) {
+  return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)x, (__bf16)y});
+}
+__device__ __forceinline__ float low_value(uint32_t pair) { return __builtin_bit_cast(float, pair << 16); }
+__device__ __forceinline__ float high_value(uint32_t pair) { return __builtin_bit_cast(float, pair & 0xFFFF0000u); }
+
+// The columns [c0, c0 + CT) of sequence b and kv head g that a workgroup computes.
+struct Tile {
+  int b, g, r0, n, c0;  // first row and number of rows of the sequence
+  bool any;             // some column exists
+};
+
+template <int CT>
+__device__ __forceinline__ Tile find_tile(const RowsAttnArgs& a, unsigned wg, int lane) {
+  const unsigned slot = a.by_hkv.quotient(wg);
+  auto first_slot = [&](int b) { return row_start(a.row_begin, b, a.rows) * a.G / CT + b; };
+  Tile t;
+  t.g = (int)(wg - slot * a.s.Hkv);
+  t.b = last_at_most(a.s.B, (int)slot, lane, first_slot);
+  t.r0 = row_start(a.row_begin, t.b, a.rows);
+  t.n = row_start(a.row_begin, t.b + 1, a.rows) - t.r0;
+  t.c0 = ((int)slot - (t.r0 * a.G / CT + t.b)) * CT;
+  t.any = t.c0 >= 0 && t.c0 < t.n * a.G;
+  return t;
+}
+
+// What one column's row sees, beside the ranges.
+template <RowsMode MODE>
+struct Sight;
+template <>
+struct Sight<RowsMode::kTree> {
+  uint64_t nodes;
+};
+template <>
+struct Sight<RowsMode::kWindow> {
+  int pos;  // -1: before the first token, sees nothing
+};
+
+// The token ranges that the rows of a tile see, one per lane, their blocks one after the other making one
+// list (a tile's rows may see parts of a range only).
 struct Ranges {
-  int t0, t1, nblk, vend;
+  int t0, t1, nblk, vend;  // this lane's: tokens, blocks, end of its blocks in the list
+  int count, total;        // ranges, blocks of all
+  int tree;                // tree: the range of the nodes
+  int tree0;               // and its first token
 
   __device__ __forceinline__ void scan(int lane) {
     nblk = t1 > t0 ? ((t1 - 1) >> 4) - (t0 >> 4) + 1 : 0;
     vend = nblk;
+    if (count > 2) {
 #pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int y = __shfl_up(vend, off);
-      if (lane >= off) vend += y;
+      for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(vend, off);
+        if (lane >= off) vend += y;
+      }
+    } else {
+      const int first = __builtin_amdgcn_readlane(nblk, 0);
+      if (lane == 1) vend += first;
     }
+    total = __builtin_amdgcn_readlane(vend, count - 1);
   }
 };
 
-// Element of a row that a token is seen by.
+// Ranges seen by the columns [ca, cb) of a tile (rows i = c / G).
 template <RowsMode MODE>
-struct Sight {
-  int pos, window, sinks;  // window: position of the row (-1: sees nothing)
-  uint64_t nodes;          // tree: the nodes it sees
-
-  __device__ __forceinline__ bool token(int t) const { return t <= pos && (t > pos - window || t < sinks); }
-  __device__ __forceinline__ bool node(int j) const { return (nodes >> (j & 63)) & 1; }
-};
-
-template <RowsMode MODE, bool BF16>
-__global__ __launch_bounds__(64) void rows_attn_kernel(RowsAttnArgs a) {
-  const int lane = threadIdx.x, col = lane & 15, quad = lane >> 4;
-  const int G = a.G, B = a.s.B;
-  const unsigned slot = a.by_hkv.quotient(blockIdx.x);
-  const int g = (int)(blockIdx.x - slot * a.s.Hkv);
-  auto first_slot = [&](int b) { return row_start(a.row_begin, b, a.rows) * G / kCols + b; };
-  const int b = last_at_most(B, (int)slot, lane, first_slot);
-  const int r0 = row_start(a.row_begin, b, a.rows);
-  const int n = row_start(a.row_begin, b + 1, a.rows) - r0;
-  const int c0 = ((int)slot - (r0 * G / kCols + b)) * kCols;
-  if (c0 < 0 || c0 >= n * G) return;
-
-  const int c = c0 + col;
-  const bool live = c < n * G;
-  const int i = live ? (int)a.by_g.quotient(c) : n - 1;
-  const int h = live ? c - i * G : 0;
-  const int64_t qrow = (int64_t)(r0 + i) * a.Hq + g * G + h;
-  const int span = a.s.max_blocks * kBlockSize;
-
-  // What the rows see, together and each.
-  Sight<MODE> sight;
-  Ranges rg;
-  rg.t0 = rg.t1 = 0;
-  int n_ranges;
-  int tree0 = -1;
+__device__ __forceinline__ Ranges find_ranges(const RowsAttnArgs& a, const Tile& t, int ca, int cb, int lane) {
+  Ranges r;
+  const int span = a.s.max_blocks * kBlockSize, B = a.s.B;
+  r.t0 = r.t1 = 0;
   if (MODE == RowsMode::kTree) {
-    n_ranges = a.n_parts + 1;
-    tree0 = min(a.tree_begin[b], span);
-    const int nodes = min(n, 64);
-    sight.nodes = a.mask[r0 + i];
-    if (nodes < 64) sight.nodes &= (uint64_t{1} << nodes) - 1;
+    r.count = a.n_parts + 1;
+    r.tree = a.n_parts;
+    r.tree0 = min(a.tree_begin[t.b], span);
     if (lane < a.n_parts) {
-      rg.t0 = max(a.begin[(int64_t)lane * B + b], 0);
-      rg.t1 = min(a.end[(int64_t)lane * B + b], span);
-    } else if (lane == a.n_parts && tree0 >= 0) {
-      rg.t0 = tree0;
-      rg.t1 = tree0 + min(nodes, span - tree0);
+      r.t0 = max(a.begin[(int64_t)lane * B + t.b], 0);
+      r.t1 = min(a.end[(int64_t)lane * B + t.b], span);
+    } else if (lane == a.n_parts && r.tree0 >= 0) {
+      r.t0 = r.tree0;
+      r.t1 = r.tree0 + min(min(t.n, 64), span - r.tree0);
     }
   } else {
-    n_ranges = 2;
-    const int len = min(max(a.seq_lens[b], 0), span);
-    sight.window = a.window;
-    sight.sinks = a.sinks;
-    sight.pos = max(len - n + i, -1);
-    const int i0 = (int)a.by_g.quotient(c0), i1 = (int)a.by_g.quotient(min(c0 + kCols, n * G) - 1);
-    const int p0 = max(len - n + i0, 0), p1 = max(len - n + i1, -1);
-    const int lo = a.begin != nullptr ? max(a.begin[b], 0) : 0;
-    const int hi = min(a.end != nullptr ? min(a.end[b], span) : span, p1 + 1);
-    int w0 = max(p0 - a.window + 1, lo);
-    const int s1 = min(a.sinks, hi);
-    if (w0 <= s1) w0 = lo;  // sinks and window touch: one range
-    else if (lane == 0) {
-      rg.t0 = lo;
-      rg.t1 = s1;
+    r.count = 2;
+    r.tree = r.tree0 = -1;
+    const int len = min(max(a.seq_lens[t.b], 0), span);
+    const int p0 = max(len - t.n + (int)a.by_g.quotient(ca), 0), p1 = max(len - t.n + (int)a.by_g.quotient(cb - 1), -1);
+    const int lo = a.begin != nullptr ? max(a.begin[t.b], 0) : 0;
+    const int hi = min(a.end != nullptr ? min(a.end[t.b], span) : span, p1 + 1);
+    const int w0 = max(p0 - a.window + 1, lo), s1 = min(a.sinks, hi);
+    const bool apart = w0 > s1;  // sinks and window do not touch: two ranges
+    if (lane == 0 && apart) {
+      r.t0 = lo;
+      r.t1 = s1;
     }
     if (lane == 1) {
-      rg.t0 = w0;
-      rg.t1 = hi;
+      r.t0 = apart ? w0 : lo;
+      r.t1 = hi;
     }
   }
-  rg.scan(lane);
+  r.scan(lane);
+  return r;
+}
 
-  bf16x8 qop[4];
-  const uint16_t* qsrc = a.q + qrow * kHeadDim + 8 * quad;
-#pragma unroll
-  for (int kk = 0; kk < 4; ++kk) {
-    u32x4 x = *reinterpret_cast<const u32x4*>(qsrc + 32 * kk);
-    if (!live) x = u32x4{0u, 0u, 0u, 0u};
-    qop[kk] = __builtin_bit_cast(bf16x8, x);
-  }
-  f32x4 acc[kDimTiles];
-#pragma unroll
-  for (int dt = 0; dt < kDimTiles; ++dt) acc[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float m = -INFINITY, lsum = 0.f;  // m: running max of the scores in powers of two
+// Block v of the list (wave-uniform); v does not decrease from call to call.  Past the end: the last block,
+// with nothing of it seen.
+struct Cursor {
+  int p = -1, vend = 0;  // range, end of its blocks in the list
+  int offset = 0;        // logical block of list entry v: v + offset
+  int t0 = 0, t1 = 0;    // tokens of the range
 
-  for (int p = 0; p < n_ranges; ++p) {
-    const int t0 = __builtin_amdgcn_readlane(rg.t0, p), t1 = __builtin_amdgcn_readlane(rg.t1, p);
-    const bool tree = MODE == RowsMode::kTree && p == a.n_parts;
-    for (int j = t0 >> 4; t0 < t1 && j * kBlockSize < t1; ++j) {
-      const int32_t blk = min(max(table_lookup(a.table, a.s.max_blocks, b, j), 0), a.s.last_block);
-      const int64_t tile = kv_tile(blk, g, a.s.Hkv) * kTileElems;
-      const u32x4* ksrc = reinterpret_cast<const u32x4*>(a.k + tile) + (quad * kBlockSize + col);
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kk = 0; kk < 4; ++kk)
-        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, ksrc[4 * kBlockSize * kk]), qop[kk], s,
-                                                    0, 0, 0);
-      const u32x2* vsrc = reinterpret_cast<const u32x2*>(a.v + tile + col * kBlockSize + 4 * quad);
-      u32x2 vr[kDimTiles];
-#pragma unroll
-      for (int dt = 0; dt < kDimTiles; ++dt) vr[dt] = vsrc[4 * 16 * dt];
-      bool ok[4];
-      uint32_t keep[2] = {0, 0};
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int t = j * kBlockSize + 4 * quad + e;
-        const bool in = t >= t0 && t < t1;
-        ok[e] = in && (MODE == RowsMode::kTree ? !tree || sight.node(t - tree0) : sight.token(t));
-        if (in) keep[e >> 1] |= 0xFFFFu << (16 * (e & 1));
-        s[e] = ok[e] ? s[e] * a.scale : -INFINITY;
-      }
-      bool odd = false;  // a value that is not finite: only the rows that see it may meet it
-#pragma unroll
-      for (int dt = 0; dt < kDimTiles; ++dt) {
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          vr[dt][w] &= keep[w];
-          odd |= (vr[dt][w] & 0x7F80u) == 0x7F80u || (vr[dt][w] & 0x7F800000u) == 0x7F800000u;
-        }
-      }
-      float mx = fmaxf(fmaxf(s[0], s[1]), fmaxf(s[2], s[3]));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float m_new = fmaxf(m, mx);
-      const float base = m_new == -INFINITY ? 0.f : m_new;  // nothing seen yet
-      const float alpha = __builtin_amdgcn_exp2f(m - base);
-      m = m_new;
-      float w[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = __builtin_amdgcn_exp2f(s[e] - base);
-      lsum = lsum * alpha + ((w[0] + w[1]) + (w[2] + w[3]));
-#pragma unroll
-      for (int dt = 0; dt < kDimTiles; ++dt) acc[dt] *= alpha;
-      if (__any(odd)) {
-        for (int t = 0; t < kBlockSize; ++t) {
-          const int from = (t >> 2) * 16 + col;
-          const int e = t & 3;
-          const float mine = e == 0 ? w[0] : e == 1 ? w[1] : e == 2 ? w[2] : w[3];
-          const bool seen = __shfl((int)(e == 0 ? ok[0] : e == 1 ? ok[1] : e == 2 ? ok[2] : ok[3]), from);
-          const float weight = __shfl(mine, from);
-#pragma unroll
-          for (int dt = 0; dt < kDimTiles; ++dt)
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-              const float val = bf16_value(a.v[tile + (16 * dt + 4 * quad + x) * kBlockSize + t]);
-              if (seen) acc[dt][x] += weight * val;
-            }
-        }
-        continue;
-      }
-      float rest[4] = {w[0], w[1], w[2], w[3]};
-#pragma unroll
-      for (int term = 0; term < (BF16 ? 1 : 3); ++term) {
-        uint32_t bits[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          bits[e] = bf16_bits(rest[e]);
-          rest[e] -= bf16_value(bits[e]);
-        }
-        const i16x4 pop = __builtin_bit_cast(i16x4, u32x2{bits[0] | bits[1] << 16, bits[2] | bits[3] << 16});
-#pragma unroll
-        for (int dt = 0; dt < kDimTiles; ++dt)
-          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(i16x4, vr[dt]), pop, acc[dt], 0, 0, 0);
-      }
+  __device__ __forceinline__ void seek(const Ranges& r, int v) {
+    while (v >= vend && p + 1 < r.count) {
+      ++p;
+      vend = __builtin_amdgcn_readlane(r.vend, p);
+      t0 = __builtin_amdgcn_readlane(r.t0, p);
+      t1 = __builtin_amdgcn_readlane(r.t1, p);
+      offset = (t0 >> 4) - (vend - __builtin_amdgcn_readlane(r.nblk, p));
     }
   }
+};
 
-  lsum += __shfl_xor(lsum, 16);
-  lsum += __shfl_xor(lsum, 32);
-  if (!live) return;
-  const bool empty = lsum == 0.f;
-  const float inv = empty ? 0.f : 1.0f / lsum;
+// A block of a step: its first token and the tokens of its range.
+struct Block {
+  int first, t0, t1;
+  bool tree;
+};
+
+__device__ __forceinline__ Block block_at(const Ranges& r, Cursor& c, int v) {
+  c.seek(r, v);
+  const bool past = v >= r.total;
+  return {((past ? r.total - 1 : v) + c.offset) * kBlockSize, past ? 0 : c.t0, past ? 0 : c.t1, c.p == r.tree};
+}
+
+// Blocks of the pool for list entries v, one per lane (any order); past the end those of the last entry.
+__device__ __forceinline__ int pool_blocks(const RowsAttnArgs& a, const Ranges& r, int b, int v) {
+  v = min(v, r.total - 1);
+  int offset = 0;
+  for (int p = 0; p < r.count; ++p) {
+    const int vend = __builtin_amdgcn_readlane(r.vend, p), nblk = __builtin_amdgcn_readlane(r.nblk, p);
+    if (v >= vend - nblk) offset = (__builtin_amdgcn_readlane(r.t0, p) >> 4) - (vend - nblk);
+  }
+  return min(max(a.table[(int64_t)b * a.s.max_blocks + v + offset], 0), a.s.last_block);
+}
+
+// Whether all of a block's tokens are seen by all rows at positions [p0, p1] (wave-uniform).
+template <RowsMode MODE>
+__device__ __forceinline__ bool all_seen(const RowsAttnArgs& a, const Block& c, int p0, int p1) {
+  const bool in = c.first >= c.t0 && c.first + kBlockSize <= c.t1;
+  if (MODE == RowsMode::kTree) return in && !c.tree;
+  return in && c.first + kBlockSize - 1 <= p0 && (c.first > p1 - a.window || c.first + kBlockSize <= a.sinks);
+}
+
+// Whether token t of a block is seen by a row.  (Without branches: hipcc 7.2 dropped one of the conditional
+// stores that a form with && and || led to.)
+template <RowsMode MODE>
+__device__ __forceinline__ bool seen(const RowsAttnArgs& a, const Ranges& r, const Block& c, const Sight<MODE>& s,
+                                     int t) {
+  const bool in = (t >= c.t0) & (t < c.t1);
+  if constexpr (MODE == RowsMode::kTree) {
+    return in & (!c.tree | (((uint32_t)(s.nodes >> ((t - r.tree0) & 63)) & 1u) != 0));
+  } else {
+    return in & (t <= s.pos) & ((t > s.pos - a.window) | (t < a.sinks));
+  }
+}
+
+template <RowsMode MODE>
+__device__ __forceinline__ Sight<MODE> sight_of(const RowsAttnArgs& a, const Tile& t, int i) {
+  Sight<MODE> s;
+  if constexpr (MODE == RowsMode::kTree) {
+    s.nodes = a.mask[t.r0 + i];
+    if (t.n < 64) s.nodes &= (uint64_t{1} << t.n) - 1;
+  } else {
+    s.pos = max(min(max(a.seq_lens[t.b], 0), a.s.max_blocks * kBlockSize) - t.n + i, -1);
+  }
+  return s;
+}
+
+// Final rows (or a chunk's partial rows) of one 16-column tile: lane (col, quad) has dims 16 dt + 4 quad + [0, 4).
+template <bool BF16>
+__device__ __forceinline__ void store_row(const RowsAttnArgs& a, int64_t row, const f32x4 (&acc)[kDimTiles], float l,
+                                          float m, int quad) {
+  const bool empty = l == 0.f;
+  const float inv = empty ? 0.f : 1.0f / l;
 #pragma unroll
   for (int dt = 0; dt < kDimTiles; ++dt) {
     const f32x4 o = acc[dt] * inv;
-    const int64_t at = qrow * kHeadDim + 16 * dt + 4 * quad;
+    const int64_t at = row * kHeadDim + 16 * dt + 4 * quad;
     if (BF16)
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) =
-          u32x2{bf16_bits(o[0]) | bf16_bits(o[1]) << 16, bf16_bits(o[2]) | bf16_bits(o[3]) << 16};
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
     else
       *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = o;
   }
-  if (a.lse != nullptr && quad == 0) a.lse[qrow] = empty ? -INFINITY : (m + log2f(lsum)) * kLn2;
+  if (a.lse != nullptr && quad == 0) a.lse[row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// ---- wide tiles: K and V shared through LDS ---------------------------------------------------------
+//
+// Four wavefronts of 16 NT columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
+// step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two to three
+// steps ahead) and feed the operands of all four:
+//   scores  S^T[16 tok x 16 col] per block and column tile: 4 x v_mfma_f32_16x16x32_bf16 over the 128 dims
+//   values  O^T[16 dim x 16 col] += V^T[16 dim x 32 tok] P^T[32 tok x 16 col]: the 32 tokens of the product
+//           are 4 q + i of both blocks for lane quad q, which is where the score product leaves them, so P
+//           never leaves its lane.
+// K tiles lie in LDS as in memory (a fragment is 1 KiB in lane order); of V, each 16 dims hold the first 8
+// tokens of all dims, then the last 8, so that the 8-byte reads of a fragment fall on all banks.
+//
+// The three parts of a step are independent -- scores of step i + 1, weights of step i, values of step
+// i - 1 -- so that matrix and vector units work side by side in the one wavefront per SIMD that the
+// registers allow.  The running maximum is raised only where a score exceeds it by 2^8 (the weights are then
+// at most 2^8, which changes no relative rounding), which spares most steps the rescaling of the sums.
+constexpr int kTileBytes = kTileElems * 2;
+constexpr int kRing = 4;  // steps of K and of V in LDS: 64 KiB together
+constexpr int kVRing = kRing * 2 * kTileBytes;
+constexpr float kSlack = 8.f;
+
+// 1 KiB from memory into LDS: lane l's 16 bytes at base + offset go to lds + 16 l.
+__device__ __forceinline__ void fetch_1k(const char* base, uint32_t offset, uint32_t lds) {
+  const uint64_t at = reinterpret_cast<uint64_t>(base);  // the same in all lanes
+  const uint64_t src = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+  lds = __builtin_amdgcn_readfirstlane(lds);
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(src)
+               : "memory", "m0");
+}
+
+template <RowsMode MODE, bool BF16, int NT, int W>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4))) void rows_wide_kernel(
+    RowsAttnArgs a) {
+  constexpr int CT = 16 * NT * W;
+  constexpr int kLoads = 16 / W;  // KiB of a step that a wavefront requests
+  constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight
+  __shared__ __attribute__((aligned(16))) char ring[2 * kRing * 2 * kTileBytes];  // K: [kRing][2] tiles, then V
+  __shared__ int odd_tile[kRing][W / 2];  // a requester's piece of a V tile had values that are not finite
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Tile t = find_tile<CT>(a, blockIdx.x, lane);
+  if (!t.any) return;
+  const int C = t.n * a.G;
+  const Ranges rg = find_ranges<MODE>(a, t, t.c0, min(t.c0 + CT, C), lane);
+  const int np = (rg.total + 1) >> 1;
+
+  // This wavefront's columns.
+  const int cw = t.c0 + wave * 16 * NT;
+  const bool active = cw < C;
+  int64_t row[NT];
+  bool live[NT];
+  Sight<MODE> sight[NT];
+  bf16x8 qop[NT][4];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    const int c = cw + 16 * ct + col;
+    live[ct] = c < C;
+    const int i = live[ct] ? (int)a.by_g.quotient(c) : t.n - 1;
+    const int h = live[ct] ? c - i * a.G : 0;
+    row[ct] = (int64_t)(t.r0 + i) * a.Hq + t.g * a.G + h;
+    sight[ct] = sight_of<MODE>(a, t, i);
+    const uint16_t* src = a.q + row[ct] * kHeadDim + 8 * quad;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      u32x4 x = *reinterpret_cast<const u32x4*>(src + 32 * kk);
+      if (!live[ct]) x = u32x4{0u, 0u, 0u, 0u};
+      qop[ct][kk] = __builtin_bit_cast(bf16x8, x);
+    }
+  }
+  int p0 = 0, p1 = 0, t0 = 0, t1 = 0;  // positions of the wavefront's first and last row, and of the tile's
+  if (MODE == RowsMode::kWindow) {
+    const int base = min(max(a.seq_lens[t.b], 0), a.s.max_blocks * kBlockSize) - t.n;
+    p0 = base + (int)a.by_g.quotient(min(cw, C - 1));
+    p1 = max(base + (int)a.by_g.quotient(min(cw + 16 * NT, C) - 1), 0);
+    t0 = base + (int)a.by_g.quotient(t.c0);
+    t1 = max(base + (int)a.by_g.quotient(min(t.c0 + CT, C) - 1), 0);
+  }
+
+  f32x4 acc[NT][kDimTiles];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    m[ct] = -INFINITY;
+    l[ct] = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  if (np > 0) {
+    // Requests: the first half of the wavefronts brings the K tiles of a step's blocks, the second the V tiles.
+    const bool is_v = wave >= W / 2;
+    const int x_of = wave / (W / 4) & 1, part_of = wave % (W / 4);  // block of the step, piece of its tile
+    const char* pool = reinterpret_cast<const char*>(is_v ? a.v : a.k);
+    const uint32_t lane_off = is_v ? (lane >> 5) * 512 + (lane & 15) * 32 + ((lane >> 4) & 1) * 16 : lane * 16;
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring +
+                             (is_v ? kVRing : 0) + x_of * kTileBytes + part_of * kLoads * 1024;
+    int blocks;  // of the wavefront's requests, 64 steps at a time
+    auto entry = [&](int step) __attribute__((always_inline)) {
+      if ((step & 63) == 0) blocks = pool_blocks(a, rg, t.b, 2 * (step + lane) + x_of);
+      return __builtin_amdgcn_readlane(blocks, step & 63);
+    };
+    auto request = [&](int step, int blk) __attribute__((always_inline)) {
+      const char* src = pool + kv_tile(blk, t.g, a.s.Hkv) * kTileBytes + part_of * kLoads * 1024;
+      const uint32_t lds = ring_at + (step & (kRing - 1)) * 2 * kTileBytes;
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) fetch_1k(src + 1024 * x, lane_off, lds + 1024 * x);
+    };
+    const int lead = is_v ? 2 : 3;
+    for (int x = 0; x < lead; ++x) request(x, entry(x));
+
+    f32x4 s[NT][2], snext[NT][2];
+    u32x4 pw[NT][kTerms];  // weights of step i - 1 as operands
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int term = 0; term < kTerms; ++term) pw[ct][term] = u32x4{0u, 0u, 0u, 0u};
+
+    auto scores = [&](int step) __attribute__((always_inline)) {
+      const char* kt = ring + (step & (kRing - 1)) * 2 * kTileBytes + lane * 16;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) snext[ct][0] = snext[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + x * kTileBytes + 1024 * kk);
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct)
+            snext[ct][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qop[ct][kk], snext[ct][x], 0, 0, 0);
+        }
+    };
+    auto weights = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        const float base = m[ct] == -INFINITY ? 0.f : m[ct];  // nothing seen yet
+        float sum[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float x = exp2_of(fmaf(s[ct][e >> 1][2 * (e & 1)], a.scale, -base));
+          float y = exp2_of(fmaf(s[ct][e >> 1][2 * (e & 1) + 1], a.scale, -base));
+          sum[e] = x + y;
+          pw[ct][0][e] = bf16_pair(x, y);
+          if constexpr (kTerms == 3) {
+            x -= low_value(pw[ct][0][e]), y -= high_value(pw[ct][0][e]);
+            pw[ct][1][e] = bf16_pair(x, y);
+            x -= low_value(pw[ct][1][e]), y -= high_value(pw[ct][1][e]);
+            pw[ct][2][e] = bf16_pair(x, y);
+          }
+        }
+        l[ct] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+      }
+    };
+    auto values = [&](int step) __attribute__((always_inline)) {
+      const char* vt = ring + kVRing + (step & (kRing - 1)) * 2 * kTileBytes + (quad >> 1) * 256 + col * 16 +
+                       (quad & 1) * 8;
+#pragma unroll
+      for (int dt = 0; dt < kDimTiles; ++dt) {
+        const u32x2 v0 = *reinterpret_cast<const u32x2*>(vt + 512 * dt);
+        const u32x2 v1 = *reinterpret_cast<const u32x2*>(vt + kTileBytes + 512 * dt);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+          for (int term = 0; term < kTerms; ++term)
+            acc[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[ct][term]),
+                                                                  acc[ct][dt], 0, 0, 0);
+      }
+    };
+    // A V tile that not every row sees whole, before the products read it: tokens outside the range are cleared
+    // (their slots may hold anything), and values that are not finite too, as a weight of 0 would not keep them
+    // from the rows that do not see them.  Whether there were any: the rows that do see them take them one by one.
+    auto clean = [&](int step, int first, int from, int end) __attribute__((always_inline)) {
+      char* vt = ring + kVRing + (step & (kRing - 1)) * 2 * kTileBytes + x_of * kTileBytes + part_of * kLoads * 1024;
+      bool odd = false;
+#pragma unroll
+      for (int x = 0; x < kLoads; ++x) {
+        u32x4* at = reinterpret_cast<u32x4*>(vt + 1024 * x + 16 * lane);  // 8 tokens of one dim
+        u32x4 val = *at;
+        const int tok = first + ((lane >> 4) & 1) * 8;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int u = tok + 2 * e;
+          val[e] &= (u >= from && u < end ? 0x0000FFFFu : 0u) | (u + 1 >= from && u + 1 < end ? 0xFFFF0000u : 0u);
+          if ((val[e] & 0x7F80u) == 0x7F80u) val[e] &= 0xFFFF0000u, odd = true;
+          if ((val[e] & 0x7F800000u) == 0x7F800000u) val[e] &= 0x0000FFFFu, odd = true;
+        }
+        *at = val;
+      }
+      const bool any = __any(odd);
+      if (lane == 0) odd_tile[step & (kRing - 1)][wave - W / 2] = any;
+    };
+    auto odd_values = [&](Block c, int x) __attribute__((always_inline)) {
+      const int blk_of = min(max(table_lookup(a.table, a.s.max_blocks, t.b, c.first >> 4), 0), a.s.last_block);
+      const uint16_t* vt = a.v + kv_tile(blk_of, t.g, a.s.Hkv) * kTileElems;
+#pragma unroll 1
+      for (int slot = 0; slot < kBlockSize; ++slot) {
+        const int tok = c.first + slot, from = (slot >> 2) * 16 + col;
+        if (tok < c.t0 || tok >= c.t1) continue;
+        float w[NT];
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) {
+          w[ct] = 0.f;
+#pragma unroll
+          for (int term = 0; term < kTerms; ++term) {
+            const uint32_t w0 = pw[ct][term][0], w1 = pw[ct][term][1], w2 = pw[ct][term][2], w3 = pw[ct][term][3];
+            const uint32_t lo = x ? w2 : w0, hi = x ? w3 : w1;
+            const uint32_t pair = (uint32_t)__shfl((int)(slot & 2 ? hi : lo), from);
+            w[ct] += slot & 1 ? high_value(pair) : low_value(pair);
+          }
+          if (!seen<MODE>(a, rg, c, sight[ct], tok)) w[ct] = -1.f;
+        }
+#pragma unroll
+        for (int dt = 0; dt < kDimTiles; ++dt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = vt[(16 * dt + 4 * quad + e) * kBlockSize + slot];
+            if ((bits & 0x7F80u) != 0x7F80u) continue;
+#pragma unroll
+            for (int ct = 0; ct < NT; ++ct)
+              if (!(w[ct] < 0.f)) acc[ct][dt][e] += w[ct] * low_value(bits);
+          }
+      }
+    };
+
+    Cursor at;
+    Block now0, now1, before0, before1;   // the blocks of steps i and i - 1
+    bool part = false, part_now = false;  // one of them is not seen whole by all rows of the tile
+    auto begin = [&](int i) __attribute__((always_inline)) {
+      // Everybody's K tiles of step i + 1 and V tiles of step i - 1 are there, and nobody reads the tiles that
+      // are overwritten next (K of step i - 1, V of step i - 2).
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
+      request(i + lead, entry(i + lead));
+      part = part_now;
+      before0 = now0;
+      before1 = now1;
+      now0 = block_at(rg, at, 2 * i);
+      now1 = block_at(rg, at, 2 * i + 1);
+      part_now = !all_seen<MODE>(a, now0, t0, t1) || !all_seen<MODE>(a, now1, t0, t1);
+      if (is_v && part_now)
+        clean(i, x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);  // its own request of step i has arrived
+    };
+    auto odd_ones = [&](int step) __attribute__((always_inline)) {
+      bool any0 = false, any1 = false;
+      for (int y = 0; y < W / 4; ++y) {
+        any0 |= odd_tile[step & (kRing - 1)][y] != 0;
+        any1 |= odd_tile[step & (kRing - 1)][W / 4 + y] != 0;
+      }
+#pragma unroll 1
+      for (int x = any0 ? 0 : 1; x < (any1 ? 2 : 1); ++x) odd_values(x ? before1 : before0, x);
+    };
+    float top[NT];
+    auto exceeds = [&]() __attribute__((always_inline)) {  // the scores of step i are in snext
+      bool raise = false;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        s[ct][0] = snext[ct][0], s[ct][1] = snext[ct][1];
+        top[ct] = s[ct][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
+        raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
+      }
+      return __any(raise);
+    };
+    // The values of "step -1" meet weights of 0.
+    for (int x = threadIdx.x; x < 2 * kTileBytes / 16; x += 64 * W)
+      *reinterpret_cast<u32x4*>(ring + kVRing + (kRing - 1) * 2 * kTileBytes + 16 * x) = u32x4{0u, 0u, 0u, 0u};
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
+    int i = 0;
+    if (active) {
+      scores(0);
+      begin(0);
+      for (;;) {
+        // A step of any kind.
+        if (part_now && !(all_seen<MODE>(a, now0, p0, p1) && all_seen<MODE>(a, now1, p0, p1))) {
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const Block& c = e < 4 ? now0 : now1;
+              const bool ok = seen<MODE>(a, rg, c, sight[ct], c.first + 4 * quad + (e & 3));
+              snext[ct][e >> 2][e & 3] = ok ? snext[ct][e >> 2][e & 3] : -INFINITY;
+            }
+        }
+        if (part) odd_ones(i - 1);
+        values(i - 1);
+        if (exceeds()) {
+#pragma unroll
+          for (int ct = 0; ct < NT; ++ct) {
+            float x = top[ct] * a.scale;
+            x = fmaxf(x, __shfl_xor(x, 16));
+            x = fmaxf(x, __shfl_xor(x, 32));
+            const float m_new = fmaxf(m[ct], x);
+            const float alpha = exp2_of(m[ct] - (m_new == -INFINITY ? 0.f : m_new));
+            m[ct] = m_new;
+            l[ct] *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] *= alpha;
+          }
+        }
+        scores(min(i + 1, np - 1));
+        weights();
+        if (++i == np) break;
+        begin(i);
+        // Steps that every row sees whole, with no new maximum: what most steps are.
+        while (!part && !part_now && !exceeds()) {
+          scores(min(i + 1, np - 1));
+          values(i - 1);
+          weights();
+          if (++i == np) break;
+          begin(i);
+        }
+        if (i == np) break;
+      }
+    } else {
+      for (; i < np; ++i) begin(i);
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if (active) {
+      before0 = now0;
+      before1 = now1;
+      if (part_now) odd_ones(np - 1);
+      values(np - 1);
+    }
+  }
+
+  if (!active) return;
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    float sum = l[ct];
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (live[ct]) store_row<BF16>(a, row[ct], acc[ct], sum, m[ct], quad);
+  }
+}
+
+template <RowsMode MODE, bool BF16>
+void launch_wide(const RowsAttnArgs& a, hipStream_t stream) {
+#ifndef BANA_NT
+#define BANA_NT 2
+#define BANA_W 8
+#endif
+  constexpr int CT = 16 * BANA_NT * BANA_W;
+  const unsigned slots = (unsigned)((int64_t)a.rows * a.G / CT + a.s.B);
+  hipLaunchKernelGGL((rows_wide_kernel<MODE, BF16, BANA_NT, BANA_W>), dim3(slots * (unsigned)a.s.Hkv), dim3(64 * BANA_W), 0,
+                     stream, a);
 }
 
 }  // namespace
 
 hipError_t launch_rows_attn(const RowsAttnArgs& a, RowsMode mode, bool bf16, hipStream_t stream) {
-  const unsigned slots = (unsigned)((int64_t)a.rows * a.G / kCols + a.s.B);
-  const dim3 grid(slots * (unsigned)a.s.Hkv), block(64);
   if (mode == RowsMode::kTree) {
-    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, false>), grid, block, 0, stream, a);
+    if (bf16) launch_wide<RowsMode::kTree, true>(a, stream);
+    else launch_wide<RowsMode::kTree, false>(a, stream);
   } else {
-    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, false>), grid, block, 0, stream, a);
+    if (bf16) launch_wide<RowsMode::kWindow, true>(a, stream);
+    else launch_wide<RowsMode::kWindow, false>(a, stream);
   }
   return hipGetLastError();
 }
