@@ -234,21 +234,29 @@ __device__ __forceinline__ void store_row(const RowsAttnArgs& a, int64_t row, co
 // Four wavefronts of 16 NT columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
 // step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two to three
 // steps ahead) and feed the operands of all four:
-//   scores  S^T[16 tok x 16 col] per block and column tile: 4 x v_mfma_f32_16x16x32_bf16 over the 128 dims
-//   values  O^T[16 dim x 16 col] += V^T[16 dim x 32 tok] P^T[32 tok x 16 col]: the 32 tokens of the product
-//           are 4 q + i of both blocks for lane quad q, which is where the score product leaves them, so P
-//           never leaves its lane.
-// K tiles lie in LDS as in memory (a fragment is 1 KiB in lane order); of V, each 16 dims hold the first 8
-// tokens of all dims, then the last 8, so that the 8-byte reads of a fragment fall on all banks.
+//   scores  S^T[16 tok x 16 col] twice per column tile: 4 x v_mfma_f32_16x16x32_bf16 over the 128 dims
+//   values  O^T[16 dim x 16 col] += V^T[16 dim x 32 tok] P^T[32 tok x 16 col]
+// Lane quad q of the value product takes 8 consecutive tokens: slots 8 (q & 1) + [0, 8) of block q >> 1.  The
+// rows of the two score products are assigned to tokens so that they leave exactly these 8 in that quad (row
+// 4 q + i of product x: slot 8 (q & 1) + 4 x + i of block q >> 1), so P never leaves its lane.
+// A fragment is read with one 16-byte read per lane, no two lanes on the same bank: the second block's K tile
+// lies 64 bytes off (its rows fall between the first block's); of V, each 16 dims hold the first 8 tokens of
+// all dims, then the last 8.
 //
-// The three parts of a step are independent -- scores of step i + 1, weights of step i, values of step
-// i - 1 -- so that matrix and vector units work side by side in the one wavefront per SIMD that the
-// registers allow.  The running maximum is raised only where a score exceeds it by 2^8 (the weights are then
-// at most 2^8, which changes no relative rounding), which spares most steps the rescaling of the sums.
+// The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
+// changes no relative rounding), which spares most steps the rescaling of the sums.
+#ifndef BANA_NT
+#define BANA_NT 3
+#define BANA_W 4
+#define BANA_EU 2
+#endif
 constexpr int kTileBytes = kTileElems * 2;
-constexpr int kRing = 4;  // steps of K and of V in LDS: 64 KiB together
-constexpr int kVRing = kRing * 2 * kTileBytes;
+constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
+constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
+constexpr int kVStep = 2 * kTileBytes;
+constexpr int kStep = kKStep + kVStep;          // K, then V
 constexpr float kSlack = 8.f;
+
 
 // 1 KiB from memory into LDS: lane l's 16 bytes at base + offset go to lds + 16 l.
 __device__ __forceinline__ void fetch_1k(const char* base, uint32_t offset, uint32_t lds) {
@@ -261,13 +269,13 @@ __device__ __forceinline__ void fetch_1k(const char* base, uint32_t offset, uint
 }
 
 template <RowsMode MODE, bool BF16, int NT, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W / 4))) void rows_wide_kernel(
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU, BANA_EU))) void rows_wide_kernel(
     RowsAttnArgs a) {
   constexpr int CT = 16 * NT * W;
   constexpr int kLoads = 16 / W;  // KiB of a step that a wavefront requests
   constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight
-  __shared__ __attribute__((aligned(16))) char ring[2 * kRing * 2 * kTileBytes];  // K: [kRing][2] tiles, then V
-  __shared__ int odd_tile[kRing][W / 2];  // a requester's piece of a V tile had values that are not finite
+  __shared__ __attribute__((aligned(16))) char ring[kRing * kStep];
+  __shared__ int odd_tile[W / 2];  // a requester's piece of a V tile had values that are not finite
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const Tile t = find_tile<CT>(a, blockIdx.x, lane);
@@ -325,40 +333,38 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
     const char* pool = reinterpret_cast<const char*>(is_v ? a.v : a.k);
     const uint32_t lane_off = is_v ? (lane >> 5) * 512 + (lane & 15) * 32 + ((lane >> 4) & 1) * 16 : lane * 16;
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring +
-                             (is_v ? kVRing : 0) + x_of * kTileBytes + part_of * kLoads * 1024;
+                             (is_v ? kKStep : 64 * x_of) + x_of * kTileBytes + part_of * kLoads * 1024;
     int blocks;  // of the wavefront's requests, 64 steps at a time
     auto entry = [&](int step) __attribute__((always_inline)) {
       if ((step & 63) == 0) blocks = pool_blocks(a, rg, t.b, 2 * (step + lane) + x_of);
       return __builtin_amdgcn_readlane(blocks, step & 63);
     };
-    auto request = [&](int step, int blk) __attribute__((always_inline)) {
+    auto request = [&](int step, int at) __attribute__((always_inline)) {  // into the ring at byte `at`
+      const int blk = entry(step);
       const char* src = pool + kv_tile(blk, t.g, a.s.Hkv) * kTileBytes + part_of * kLoads * 1024;
-      const uint32_t lds = ring_at + (step & (kRing - 1)) * 2 * kTileBytes;
+      const uint32_t lds = ring_at + at;
 #pragma unroll
       for (int x = 0; x < kLoads; ++x) fetch_1k(src + 1024 * x, lane_off, lds + 1024 * x);
     };
-    const int lead = is_v ? 2 : 3;
-    for (int x = 0; x < lead; ++x) request(x, entry(x));
+    request(0, 0);
+    request(1, kStep);
+    f32x4 s[NT][2];
+    u32x4 pw[NT][kTerms];  // weights of the step as operands
+    int cur = 0;           // the step's place in the ring
 
-    f32x4 s[NT][2], snext[NT][2];
-    u32x4 pw[NT][kTerms];  // weights of step i - 1 as operands
+    auto scores = [&]() __attribute__((always_inline)) {
+      const char* kt = ring + cur + (col >> 3) * (kTileBytes + 64) + quad * 256 +
+                       (8 * ((col >> 2) & 1) + (col & 3)) * 16;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int term = 0; term < kTerms; ++term) pw[ct][term] = u32x4{0u, 0u, 0u, 0u};
-
-    auto scores = [&](int step) __attribute__((always_inline)) {
-      const char* kt = ring + (step & (kRing - 1)) * 2 * kTileBytes + lane * 16;
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) snext[ct][0] = snext[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int ct = 0; ct < NT; ++ct) s[ct][0] = s[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + x * kTileBytes + 1024 * kk);
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + 64 * x + 1024 * kk);
 #pragma unroll
           for (int ct = 0; ct < NT; ++ct)
-            snext[ct][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qop[ct][kk], snext[ct][x], 0, 0, 0);
+            s[ct][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qop[ct][kk], s[ct][x], 0, 0, 0);
         }
     };
     auto weights = [&]() __attribute__((always_inline)) {
@@ -382,14 +388,12 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
         l[ct] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
     };
-    auto values = [&](int step) __attribute__((always_inline)) {
-      const char* vt = ring + kVRing + (step & (kRing - 1)) * 2 * kTileBytes + (quad >> 1) * 256 + col * 16 +
-                       (quad & 1) * 8;
+    auto values = [&]() __attribute__((always_inline)) {
+      const char* vt = ring + cur + kKStep + (quad >> 1) * kTileBytes + (quad & 1) * 256 +
+                       col * 16;
 #pragma unroll
       for (int dt = 0; dt < kDimTiles; ++dt) {
-        const u32x2 v0 = *reinterpret_cast<const u32x2*>(vt + 512 * dt);
-        const u32x2 v1 = *reinterpret_cast<const u32x2*>(vt + kTileBytes + 512 * dt);
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{v0[0], v0[1], v1[0], v1[1]});
+        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(vt + 512 * dt);
 #pragma unroll
         for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
@@ -401,8 +405,8 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
     // A V tile that not every row sees whole, before the products read it: tokens outside the range are cleared
     // (their slots may hold anything), and values that are not finite too, as a weight of 0 would not keep them
     // from the rows that do not see them.  Whether there were any: the rows that do see them take them one by one.
-    auto clean = [&](int step, int first, int from, int end) __attribute__((always_inline)) {
-      char* vt = ring + kVRing + (step & (kRing - 1)) * 2 * kTileBytes + x_of * kTileBytes + part_of * kLoads * 1024;
+    auto clean = [&](int first, int from, int end) __attribute__((always_inline)) {
+      char* vt = ring + cur + kKStep + x_of * kTileBytes + part_of * kLoads * 1024;
       bool odd = false;
 #pragma unroll
       for (int x = 0; x < kLoads; ++x) {
@@ -419,14 +423,14 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
         *at = val;
       }
       const bool any = __any(odd);
-      if (lane == 0) odd_tile[step & (kRing - 1)][wave - W / 2] = any;
+      if (lane == 0) odd_tile[wave - W / 2] = any;
     };
     auto odd_values = [&](Block c, int x) __attribute__((always_inline)) {
       const int blk_of = min(max(table_lookup(a.table, a.s.max_blocks, t.b, c.first >> 4), 0), a.s.last_block);
       const uint16_t* vt = a.v + kv_tile(blk_of, t.g, a.s.Hkv) * kTileElems;
 #pragma unroll 1
       for (int slot = 0; slot < kBlockSize; ++slot) {
-        const int tok = c.first + slot, from = (slot >> 2) * 16 + col;
+        const int tok = c.first + slot, from = (2 * x + (slot >> 3)) * 16 + col;
         if (tok < c.t0 || tok >= c.t1) continue;
         float w[NT];
 #pragma unroll
@@ -435,7 +439,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
 #pragma unroll
           for (int term = 0; term < kTerms; ++term) {
             const uint32_t w0 = pw[ct][term][0], w1 = pw[ct][term][1], w2 = pw[ct][term][2], w3 = pw[ct][term][3];
-            const uint32_t lo = x ? w2 : w0, hi = x ? w3 : w1;
+            const uint32_t lo = slot & 4 ? w2 : w0, hi = slot & 4 ? w3 : w1;
             const uint32_t pair = (uint32_t)__shfl((int)(slot & 2 ? hi : lo), from);
             w[ct] += slot & 1 ? high_value(pair) : low_value(pair);
           }
@@ -454,68 +458,48 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
       }
     };
 
-    Cursor at;
-    Block now0, now1, before0, before1;   // the blocks of steps i and i - 1
-    bool part = false, part_now = false;  // one of them is not seen whole by all rows of the tile
+    Cursor walk;
+    Block now0, now1;  // the step's blocks
+    bool part;         // one of them is not seen whole by all rows of the tile
     auto begin = [&](int i) __attribute__((always_inline)) {
-      // Everybody's K tiles of step i + 1 and V tiles of step i - 1 are there, and nobody reads the tiles that
-      // are overwritten next (K of step i - 1, V of step i - 2).
+      // Everybody's tiles of this step are there, and nobody reads those of the step before.
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-      request(i + lead, entry(i + lead));
-      part = part_now;
-      before0 = now0;
-      before1 = now1;
-      now0 = block_at(rg, at, 2 * i);
-      now1 = block_at(rg, at, 2 * i + 1);
-      part_now = !all_seen<MODE>(a, now0, t0, t1) || !all_seen<MODE>(a, now1, t0, t1);
-      if (is_v && part_now)
-        clean(i, x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);  // its own request of step i has arrived
-    };
-    auto odd_ones = [&](int step) __attribute__((always_inline)) {
-      bool any0 = false, any1 = false;
-      for (int y = 0; y < W / 4; ++y) {
-        any0 |= odd_tile[step & (kRing - 1)][y] != 0;
-        any1 |= odd_tile[step & (kRing - 1)][W / 4 + y] != 0;
+      request(i + 2, cur == 0 ? 2 * kStep : cur - kStep);
+      now0 = block_at(rg, walk, 2 * i);
+      now1 = block_at(rg, walk, 2 * i + 1);
+      part = !all_seen<MODE>(a, now0, t0, t1) || !all_seen<MODE>(a, now1, t0, t1);
+      if (part) {
+        if (is_v) clean(x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
       }
-#pragma unroll 1
-      for (int x = any0 ? 0 : 1; x < (any1 ? 2 : 1); ++x) odd_values(x ? before1 : before0, x);
     };
-    float top[NT];
-    auto exceeds = [&]() __attribute__((always_inline)) {  // the scores of step i are in snext
-      bool raise = false;
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        s[ct][0] = snext[ct][0], s[ct][1] = snext[ct][1];
-        top[ct] = s[ct][0][0];
-#pragma unroll
-        for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
-        raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
-      }
-      return __any(raise);
-    };
-    // The values of "step -1" meet weights of 0.
-    for (int x = threadIdx.x; x < 2 * kTileBytes / 16; x += 64 * W)
-      *reinterpret_cast<u32x4*>(ring + kVRing + (kRing - 1) * 2 * kTileBytes + 16 * x) = u32x4{0u, 0u, 0u, 0u};
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * kLoads) : "memory");
-    int i = 0;
     if (active) {
-      scores(0);
-      begin(0);
-      for (;;) {
-        // A step of any kind.
-        if (part_now && !(all_seen<MODE>(a, now0, p0, p1) && all_seen<MODE>(a, now1, p0, p1))) {
+#pragma unroll 1
+      for (int i = 0; i < np; ++i) {
+        begin(i);
+        scores();
+        if (part && !(all_seen<MODE>(a, now0, p0, p1) && all_seen<MODE>(a, now1, p0, p1))) {
+          const bool second = quad >= 2;  // this lane's block
+          const Block mine = {second ? now1.first : now0.first, second ? now1.t0 : now0.t0,
+                              second ? now1.t1 : now0.t1, second ? now1.tree : now0.tree};
 #pragma unroll
           for (int ct = 0; ct < NT; ++ct)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-              const Block& c = e < 4 ? now0 : now1;
-              const bool ok = seen<MODE>(a, rg, c, sight[ct], c.first + 4 * quad + (e & 3));
-              snext[ct][e >> 2][e & 3] = ok ? snext[ct][e >> 2][e & 3] : -INFINITY;
+              const bool ok = seen<MODE>(a, rg, mine, sight[ct], mine.first + 8 * (quad & 1) + e);
+              s[ct][e >> 2][e & 3] = ok ? s[ct][e >> 2][e & 3] : -INFINITY;
             }
         }
-        if (part) odd_ones(i - 1);
-        values(i - 1);
-        if (exceeds()) {
+        float top[NT];
+        bool raise = false;
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) {
+          top[ct] = s[ct][0][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
+          raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
+        }
+        if (__any(raise)) {
 #pragma unroll
           for (int ct = 0; ct < NT; ++ct) {
             float x = top[ct] * a.scale;
@@ -529,30 +513,27 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
             for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] *= alpha;
           }
         }
-        scores(min(i + 1, np - 1));
         weights();
-        if (++i == np) break;
-        begin(i);
-        // Steps that every row sees whole, with no new maximum: what most steps are.
-        while (!part && !part_now && !exceeds()) {
-          scores(min(i + 1, np - 1));
-          values(i - 1);
-          weights();
-          if (++i == np) break;
-          begin(i);
+        if (part) {
+          bool any0 = false, any1 = false;
+          for (int y = 0; y < W / 4; ++y) {
+            any0 |= odd_tile[y] != 0;
+            any1 |= odd_tile[W / 4 + y] != 0;
+          }
+#pragma unroll 1
+          for (int x = any0 ? 0 : 1; x < (any1 ? 2 : 1); ++x) odd_values(x ? now1 : now0, x);
         }
-        if (i == np) break;
+        values();
+        cur = cur == 2 * kStep ? 0 : cur + kStep;
       }
     } else {
-      for (; i < np; ++i) begin(i);
+#pragma unroll 1
+      for (int i = 0; i < np; ++i) {
+        begin(i);
+        cur = cur == 2 * kStep ? 0 : cur + kStep;
+      }
     }
-    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    if (active) {
-      before0 = now0;
-      before1 = now1;
-      if (part_now) odd_ones(np - 1);
-      values(np - 1);
-    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no request outlives the workgroup's LDS
   }
 
   if (!active) return;
@@ -567,10 +548,6 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(W / 4, W
 
 template <RowsMode MODE, bool BF16>
 void launch_wide(const RowsAttnArgs& a, hipStream_t stream) {
-#ifndef BANA_NT
-#define BANA_NT 2
-#define BANA_W 8
-#endif
   constexpr int CT = 16 * BANA_NT * BANA_W;
   const unsigned slots = (unsigned)((int64_t)a.rows * a.G / CT + a.s.B);
   hipLaunchKernelGGL((rows_wide_kernel<MODE, BF16, BANA_NT, BANA_W>), dim3(slots * (unsigned)a.s.Hkv), dim3(64 * BANA_W), 0,
