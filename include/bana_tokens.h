@@ -56,7 +56,8 @@ extern "C" {
  * workspace: optional, bana_tree_attn_workspace_bytes bytes let the library split long
  * ranges over workgroups (with less the call runs unsplit, the same result up to rounding).  Calls that may overlap must not
  * share one; its contents need no initialisation.  Results are bit-identical run to run for the same
- * inputs and dims.  BANA_ERR_UNSUPPORTED: rows x num_q_heads of 2^26 or more, n_parts above 63, n_parts * max_blocks_per_seq above 2^30.
+ * inputs and dims.  BANA_ERR_UNSUPPORTED: rows of 2^24 or rows * num_q_heads
+ * of 2^26 or more, batch * num_kv_heads above 2^23, n_parts above 63, n_parts * max_blocks_per_seq above 2^30.
  */
 bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_begin, const void* q,
                            const void* k_cache, const void* v_cache, const int32_t* block_table,

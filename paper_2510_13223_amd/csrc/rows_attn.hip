@@ -137,32 +137,45 @@ __device__ __forceinline__ Ranges find_ranges(const RowsAttnArgs& a, const Tile&
   return r;
 }
 
-// Block v of the list (wave-uniform); v does not decrease from call to call.  Past the end: the last block,
-// with nothing of it seen.
+// The range that holds block v of the list (wave-uniform; v does not decrease from call to call), and which
+// of its blocks are seen whole by all rows at positions [p0, p1].
 struct Cursor {
-  int p = -1, vend = 0;  // range, end of its blocks in the list
-  int offset = 0;        // logical block of list entry v: v + offset
-  int t0 = 0, t1 = 0;    // tokens of the range
+  int p = -1, vend = 0;    // range, end of its blocks in the list
+  int offset = 0;          // logical block of list entry v: v + offset
+  int t0 = 0, t1 = 0;      // tokens of the range
+  int wbegin = 0, wend = 0;  // list entries seen whole
 
-  __device__ __forceinline__ void seek(const Ranges& r, int v) {
+  template <RowsMode MODE>
+  __device__ __forceinline__ void seek(const RowsAttnArgs& a, const Ranges& r, int v, int p0, int p1) {
     while (v >= vend && p + 1 < r.count) {
       ++p;
       vend = __builtin_amdgcn_readlane(r.vend, p);
       t0 = __builtin_amdgcn_readlane(r.t0, p);
       t1 = __builtin_amdgcn_readlane(r.t1, p);
       offset = (t0 >> 4) - (vend - __builtin_amdgcn_readlane(r.nblk, p));
+      int from = t0, end = t1;
+      if (MODE == RowsMode::kTree) {
+        if (p == r.tree) end = from;
+      } else {
+        end = min(t1, p0 + 1);
+        if (p == 1) from = max(t0, p1 - a.window + 1);
+      }
+      wbegin = ((from + kBlockSize - 1) >> 4) - offset;
+      wend = (end >> 4) - offset;
     }
   }
 };
 
-// A block of a step: its first token and the tokens of its range.
+// A block of a step: its first token and the tokens of its range.  Past the list's end: the last block, with
+// nothing of it seen.
 struct Block {
   int first, t0, t1;
   bool tree;
 };
 
-__device__ __forceinline__ Block block_at(const Ranges& r, Cursor& c, int v) {
-  c.seek(r, v);
+template <RowsMode MODE>
+__device__ __forceinline__ Block block_at(const RowsAttnArgs& a, const Ranges& r, Cursor& c, int v, int p0, int p1) {
+  c.seek<MODE>(a, r, v, p0, p1);
   const bool past = v >= r.total;
   return {((past ? r.total - 1 : v) + c.offset) * kBlockSize, past ? 0 : c.t0, past ? 0 : c.t1, c.p == r.tree};
 }
@@ -176,14 +189,6 @@ __device__ __forceinline__ int pool_blocks(const RowsAttnArgs& a, const Ranges& 
     if (v >= vend - nblk) offset = (__builtin_amdgcn_readlane(r.t0, p) >> 4) - (vend - nblk);
   }
   return min(max(a.table[(int64_t)b * a.s.max_blocks + v + offset], 0), a.s.last_block);
-}
-
-// Whether all of a block's tokens are seen by all rows at positions [p0, p1] (wave-uniform).
-template <RowsMode MODE>
-__device__ __forceinline__ bool all_seen(const RowsAttnArgs& a, const Block& c, int p0, int p1) {
-  const bool in = c.first >= c.t0 && c.first + kBlockSize <= c.t1;
-  if (MODE == RowsMode::kTree) return in && !c.tree;
-  return in && c.first + kBlockSize - 1 <= p0 && (c.first > p1 - a.window || c.first + kBlockSize <= a.sinks);
 }
 
 // Whether token t of a block is seen by a row.  (Without branches: hipcc 7.2 dropped one of the conditional
@@ -211,10 +216,10 @@ __device__ __forceinline__ Sight<MODE> sight_of(const RowsAttnArgs& a, const Til
   return s;
 }
 
-// Final rows (or a chunk's partial rows) of one 16-column tile: lane (col, quad) has dims 16 dt + 4 quad + [0, 4).
+// Rows of one 16-column tile: lane (col, quad) has dims 16 dt + 4 quad + [0, 4).  m in powers of two.
 template <bool BF16>
-__device__ __forceinline__ void store_row(const RowsAttnArgs& a, int64_t row, const f32x4 (&acc)[kDimTiles], float l,
-                                          float m, int quad) {
+__device__ __forceinline__ void store_row(void* __restrict__ out, float* __restrict__ lse, int64_t row,
+                                          const f32x4 (&acc)[kDimTiles], float l, float m, int quad) {
   const bool empty = l == 0.f;
   const float inv = empty ? 0.f : 1.0f / l;
 #pragma unroll
@@ -222,16 +227,16 @@ __device__ __forceinline__ void store_row(const RowsAttnArgs& a, int64_t row, co
     const f32x4 o = acc[dt] * inv;
     const int64_t at = row * kHeadDim + 16 * dt + 4 * quad;
     if (BF16)
-      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + at) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
     else
-      *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + at) = o;
+      *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = o;
   }
-  if (a.lse != nullptr && quad == 0) a.lse[row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (lse != nullptr && quad == 0) lse[row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// ---- wide tiles: K and V shared through LDS ---------------------------------------------------------
+// ---- the kernel: K and V shared through LDS ---------------------------------------------------------
 //
-// Four wavefronts of 16 NT columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
+// Four wavefronts of 32 columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
 // step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two to three
 // steps ahead) and feed the operands of all four:
 //   scores  S^T[16 tok x 16 col] twice per column tile: 4 x v_mfma_f32_16x16x32_bf16 over the 128 dims
@@ -245,44 +250,57 @@ __device__ __forceinline__ void store_row(const RowsAttnArgs& a, int64_t row, co
 //
 // The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
 // changes no relative rounding), which spares most steps the rescaling of the sums.
-#ifndef BANA_NT
-#define BANA_NT 3
-#define BANA_W 4
-#define BANA_EU 2
-#endif
 constexpr int kTileBytes = kTileElems * 2;
-constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
+#ifndef BANA_RING
+#define BANA_RING 3
+#define BANA_EU (BF16 ? 3 : 2)
+#endif
+constexpr int kRing = BANA_RING;
 constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
 constexpr int kVStep = 2 * kTileBytes;
 constexpr int kStep = kKStep + kVStep;          // K, then V
 constexpr float kSlack = 8.f;
+constexpr int NT = 2, W = 4;      // column tiles of a wavefront, wavefronts
+constexpr int CT = 16 * NT * W;  // columns of a workgroup
+static_assert(CT == kRowsTile, "the planner's tile");
 
 
-// 1 KiB from memory into LDS: lane l's 16 bytes at base + offset go to lds + 16 l.
-__device__ __forceinline__ void fetch_1k(const char* base, uint32_t offset, uint32_t lds) {
-  const uint64_t at = reinterpret_cast<uint64_t>(base);  // the same in all lanes
-  const uint64_t src = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 |
-                       (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
-  lds = __builtin_amdgcn_readfirstlane(lds);
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(offset), "s"(src)
-               : "memory", "m0");
+// 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.
+__device__ __forceinline__ void fetch_4k(uint64_t base, const uint32_t (&offset)[4], uint32_t lds) {
+  asm volatile(
+      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %5\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
+      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5" ::"v"(offset[0]),
+      "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(lds), "s"(base)
+      : "memory", "m0", "scc");
 }
 
-template <RowsMode MODE, bool BF16, int NT, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU, BANA_EU))) void rows_wide_kernel(
-    RowsAttnArgs a) {
-  constexpr int CT = 16 * NT * W;
-  constexpr int kLoads = 16 / W;  // KiB of a step that a wavefront requests
+struct Yes {
+  static constexpr bool value = true;
+};
+struct No {
+  static constexpr bool value = false;
+};
+
+template <RowsMode MODE, bool BF16>
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU, BANA_EU)))
+void rows_attn_kernel(RowsAttnArgs a) {
+  constexpr int kLoads = 4;           // requests of a wavefront and step, 1 KiB each
   constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight
   __shared__ __attribute__((aligned(16))) char ring[kRing * kStep];
-  __shared__ int odd_tile[W / 2];  // a requester's piece of a V tile had values that are not finite
+  __shared__ int odd_tile[2];  // a V tile had values that are not finite
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Tile t = find_tile<CT>(a, blockIdx.x, lane);
+  const unsigned chunk = a.by_tiles.quotient(blockIdx.x);
+  const Tile t = find_tile<CT>(a, blockIdx.x - chunk * a.tiles, lane);
   if (!t.any) return;
   const int C = t.n * a.G;
   const Ranges rg = find_ranges<MODE>(a, t, t.c0, min(t.c0 + CT, C), lane);
-  const int np = (rg.total + 1) >> 1;
+  // This chunk's steps [s0, s0 + np) of the list's.
+  const int steps = (rg.total + 1) >> 1;
+  const int per = max((int)(((unsigned)steps + a.nc - 1) / (unsigned)a.nc), a.least);
+  const int s0 = min((int)chunk * per, steps), np = min(per, steps - s0);
 
   // This wavefront's columns.
   const int cw = t.c0 + wave * 16 * NT;
@@ -307,13 +325,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
       qop[ct][kk] = __builtin_bit_cast(bf16x8, x);
     }
   }
-  int p0 = 0, p1 = 0, t0 = 0, t1 = 0;  // positions of the wavefront's first and last row, and of the tile's
+  int p0 = 0, p1 = 0;  // positions of the tile's first and last row
   if (MODE == RowsMode::kWindow) {
     const int base = min(max(a.seq_lens[t.b], 0), a.s.max_blocks * kBlockSize) - t.n;
-    p0 = base + (int)a.by_g.quotient(min(cw, C - 1));
-    p1 = max(base + (int)a.by_g.quotient(min(cw + 16 * NT, C) - 1), 0);
-    t0 = base + (int)a.by_g.quotient(t.c0);
-    t1 = max(base + (int)a.by_g.quotient(min(t.c0 + CT, C) - 1), 0);
+    p0 = max(base + (int)a.by_g.quotient(t.c0), -1);
+    p1 = max(base + (int)a.by_g.quotient(min(t.c0 + CT, C) - 1), 0);
   }
 
   f32x4 acc[NT][kDimTiles];
@@ -327,27 +343,29 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
   }
 
   if (np > 0) {
-    // Requests: the first half of the wavefronts brings the K tiles of a step's blocks, the second the V tiles.
-    const bool is_v = wave >= W / 2;
-    const int x_of = wave / (W / 4) & 1, part_of = wave % (W / 4);  // block of the step, piece of its tile
-    const char* pool = reinterpret_cast<const char*>(is_v ? a.v : a.k);
-    const uint32_t lane_off = is_v ? (lane >> 5) * 512 + (lane & 15) * 32 + ((lane >> 4) & 1) * 16 : lane * 16;
-    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring +
-                             (is_v ? kKStep : 64 * x_of) + x_of * kTileBytes + part_of * kLoads * 1024;
-    int blocks;  // of the wavefront's requests, 64 steps at a time
-    auto entry = [&](int step) __attribute__((always_inline)) {
-      if ((step & 63) == 0) blocks = pool_blocks(a, rg, t.b, 2 * (step + lane) + x_of);
-      return __builtin_amdgcn_readlane(blocks, step & 63);
-    };
-    auto request = [&](int step, int at) __attribute__((always_inline)) {  // into the ring at byte `at`
-      const int blk = entry(step);
-      const char* src = pool + kv_tile(blk, t.g, a.s.Hkv) * kTileBytes + part_of * kLoads * 1024;
-      const uint32_t lds = ring_at + at;
+    // Requests: wavefronts 0 and 1 bring the K tiles of a step's blocks, 2 and 3 the V tiles.
+    const bool is_v = wave >= 2;
+    const int x_of = wave & 1;  // block of the step
+    uint32_t lane_off[4];
 #pragma unroll
-      for (int x = 0; x < kLoads; ++x) fetch_1k(src + 1024 * x, lane_off, lds + 1024 * x);
+    for (int x = 0; x < 4; ++x)
+      lane_off[x] = 1024 * x + (is_v ? (lane >> 5) * 512 + (lane & 15) * 32 + ((lane >> 4) & 1) * 16 : lane * 16);
+    const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring +
+                             (is_v ? kKStep : 64 * x_of) + x_of * kTileBytes;
+    const uint64_t pool = reinterpret_cast<uint64_t>(is_v ? a.v : a.k);
+    uint32_t tile_lo = 0, tile_hi = 0;  // addresses of the wavefront's tiles, 64 steps at a time, one per lane
+    auto request = [&](int step, int at) __attribute__((always_inline)) {  // into the ring at byte `at`
+      if ((step & 63) == 0) {
+        const int blk = pool_blocks(a, rg, t.b, 2 * (s0 + step + lane) + x_of);
+        const uint64_t tile = pool + kv_tile(blk, t.g, a.s.Hkv) * kTileBytes;
+        tile_lo = (uint32_t)tile, tile_hi = (uint32_t)(tile >> 32);
+      }
+      const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(tile_hi, step & 63) << 32 |
+                            (uint32_t)__builtin_amdgcn_readlane(tile_lo, step & 63);
+      fetch_4k(base, lane_off, __builtin_amdgcn_readfirstlane(ring_at + at));
     };
-    request(0, 0);
-    request(1, kStep);
+#pragma unroll
+    for (int x = 0; x < kRing - 1; ++x) request(x, x * kStep);
     f32x4 s[NT][2];
     u32x4 pw[NT][kTerms];  // weights of the step as operands
     int cur = 0;           // the step's place in the ring
@@ -406,10 +424,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
     // (their slots may hold anything), and values that are not finite too, as a weight of 0 would not keep them
     // from the rows that do not see them.  Whether there were any: the rows that do see them take them one by one.
     auto clean = [&](int first, int from, int end) __attribute__((always_inline)) {
-      char* vt = ring + cur + kKStep + x_of * kTileBytes + part_of * kLoads * 1024;
+      char* vt = ring + cur + kKStep + x_of * kTileBytes;
       bool odd = false;
 #pragma unroll
-      for (int x = 0; x < kLoads; ++x) {
+      for (int x = 0; x < 4; ++x) {
         u32x4* at = reinterpret_cast<u32x4*>(vt + 1024 * x + 16 * lane);  // 8 tokens of one dim
         u32x4 val = *at;
         const int tok = first + ((lane >> 4) & 1) * 8;
@@ -423,7 +441,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
         *at = val;
       }
       const bool any = __any(odd);
-      if (lane == 0) odd_tile[wave - W / 2] = any;
+      if (lane == 0) odd_tile[x_of] = any;
     };
     auto odd_values = [&](Block c, int x) __attribute__((always_inline)) {
       const int blk_of = min(max(table_lookup(a.table, a.s.max_blocks, t.b, c.first >> 4), 0), a.s.last_block);
@@ -458,81 +476,86 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
       }
     };
 
-    Cursor walk;
-    Block now0, now1;  // the step's blocks
-    bool part;         // one of them is not seen whole by all rows of the tile
-    auto begin = [&](int i) __attribute__((always_inline)) {
-      // Everybody's tiles of this step are there, and nobody reads those of the step before.
-      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(kLoads) : "memory");
-      request(i + 2, cur == 0 ? 2 * kStep : cur - kStep);
-      now0 = block_at(rg, walk, 2 * i);
-      now1 = block_at(rg, walk, 2 * i + 1);
-      part = !all_seen<MODE>(a, now0, t0, t1) || !all_seen<MODE>(a, now1, t0, t1);
-      if (part) {
-        if (is_v) clean(x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    // The sums follow the maximum where a score exceeds it by more than the slack.
+    auto raise_maximum = [&]() __attribute__((always_inline)) {
+      float top[NT];
+      bool raise = false;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        top[ct] = s[ct][0][0];
+#pragma unroll
+        for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
+        raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
       }
-    };
-    if (active) {
-#pragma unroll 1
-      for (int i = 0; i < np; ++i) {
-        begin(i);
-        scores();
-        if (part && !(all_seen<MODE>(a, now0, p0, p1) && all_seen<MODE>(a, now1, p0, p1))) {
-          const bool second = quad >= 2;  // this lane's block
-          const Block mine = {second ? now1.first : now0.first, second ? now1.t0 : now0.t0,
-                              second ? now1.t1 : now0.t1, second ? now1.tree : now0.tree};
-#pragma unroll
-          for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              const bool ok = seen<MODE>(a, rg, mine, sight[ct], mine.first + 8 * (quad & 1) + e);
-              s[ct][e >> 2][e & 3] = ok ? s[ct][e >> 2][e & 3] : -INFINITY;
-            }
-        }
-        float top[NT];
-        bool raise = false;
+      if (__any(raise)) {
 #pragma unroll
         for (int ct = 0; ct < NT; ++ct) {
-          top[ct] = s[ct][0][0];
+          float x = top[ct] * a.scale;
+          x = fmaxf(x, __shfl_xor(x, 16));
+          x = fmaxf(x, __shfl_xor(x, 32));
+          const float m_new = fmaxf(m[ct], x);
+          const float alpha = exp2_of(m[ct] - (m_new == -INFINITY ? 0.f : m_new));
+          m[ct] = m_new;
+          l[ct] *= alpha;
 #pragma unroll
-          for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
-          raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
+          for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] *= alpha;
         }
-        if (__any(raise)) {
-#pragma unroll
-          for (int ct = 0; ct < NT; ++ct) {
-            float x = top[ct] * a.scale;
-            x = fmaxf(x, __shfl_xor(x, 16));
-            x = fmaxf(x, __shfl_xor(x, 32));
-            const float m_new = fmaxf(m[ct], x);
-            const float alpha = exp2_of(m[ct] - (m_new == -INFINITY ? 0.f : m_new));
-            m[ct] = m_new;
-            l[ct] *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] *= alpha;
-          }
-        }
-        weights();
-        if (part) {
-          bool any0 = false, any1 = false;
-          for (int y = 0; y < W / 4; ++y) {
-            any0 |= odd_tile[y] != 0;
-            any1 |= odd_tile[W / 4 + y] != 0;
-          }
-#pragma unroll 1
-          for (int x = any0 ? 0 : 1; x < (any1 ? 2 : 1); ++x) odd_values(x ? now1 : now0, x);
-        }
-        values();
-        cur = cur == 2 * kStep ? 0 : cur + kStep;
       }
-    } else {
+    };
+    auto next = [&](int i) __attribute__((always_inline)) {
+      // Everybody's tiles of this step are there, and nobody reads those of the step before.
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kRing - 2) * kLoads) : "memory");
+      request(i + kRing - 1, cur == 0 ? (kRing - 1) * kStep : cur - kStep);
+    };
+    auto walk = [&](auto computes) __attribute__((always_inline)) {
+      constexpr bool kComputes = decltype(computes)::value;
+      Cursor c;
+      Block now0, now1;
+      int whole = 0;  // steps from here on that all rows see whole
 #pragma unroll 1
       for (int i = 0; i < np; ++i) {
-        begin(i);
-        cur = cur == 2 * kStep ? 0 : cur + kStep;
+        next(i);
+        bool part = false;
+        if (whole == 0) {
+          const int v = 2 * (s0 + i);
+          c.seek<MODE>(a, rg, v, p0, p1);
+          if (v >= c.wbegin) whole = max((c.wend - v) >> 1, 0);
+          part = whole == 0;
+          if (part) {
+            now0 = block_at<MODE>(a, rg, c, v, p0, p1);
+            now1 = block_at<MODE>(a, rg, c, v + 1, p0, p1);
+            if (is_v) clean(x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);
+            asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+          }
+        }
+        if (!part) --whole;
+        if constexpr (kComputes) {
+          scores();
+          if (part) {
+            const bool second = quad >= 2;  // this lane's block
+            const Block mine = {second ? now1.first : now0.first, second ? now1.t0 : now0.t0,
+                                second ? now1.t1 : now0.t1, second ? now1.tree : now0.tree};
+#pragma unroll
+            for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+              for (int e = 0; e < 8; ++e) {
+                const bool ok = seen<MODE>(a, rg, mine, sight[ct], mine.first + 8 * (quad & 1) + e);
+                s[ct][e >> 2][e & 3] = ok ? s[ct][e >> 2][e & 3] : -INFINITY;
+              }
+          }
+          raise_maximum();
+          weights();
+          if (part) {
+#pragma unroll 1
+            for (int x = odd_tile[0] ? 0 : 1; x < (odd_tile[1] ? 2 : 1); ++x) odd_values(x ? now1 : now0, x);
+          }
+          values();
+        }
+        cur = cur == (kRing - 1) * kStep ? 0 : cur + kStep;
       }
-    }
+    };
+    if (active) walk(Yes{});
+    else walk(No{});
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no request outlives the workgroup's LDS
   }
 
@@ -542,28 +565,113 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU,
     float sum = l[ct];
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
-    if (live[ct]) store_row<BF16>(a, row[ct], acc[ct], sum, m[ct], quad);
+    if (!live[ct]) continue;
+    if (a.nc == 1) {
+      store_row<BF16>(a.out, a.lse, row[ct], acc[ct], sum, m[ct], quad);
+    } else if (np > 0) {  // a chunk's partial rows
+      const int64_t base = (int64_t)chunk * a.rows * a.Hq;
+      store_row<false>(a.part_out + base * kHeadDim, a.part_lse + base, row[ct], acc[ct], sum, m[ct], quad);
+    } else if (quad == 0) {
+      a.part_lse[(int64_t)chunk * a.rows * a.Hq + row[ct]] = -INFINITY;
+    }
   }
 }
 
-template <RowsMode MODE, bool BF16>
-void launch_wide(const RowsAttnArgs& a, hipStream_t stream) {
-  constexpr int CT = 16 * BANA_NT * BANA_W;
-  const unsigned slots = (unsigned)((int64_t)a.rows * a.G / CT + a.s.B);
-  hipLaunchKernelGGL((rows_wide_kernel<MODE, BF16, BANA_NT, BANA_W>), dim3(slots * (unsigned)a.s.Hkv), dim3(64 * BANA_W), 0,
-                     stream, a);
+// Merge of the chunks' partial rows (as merge.hip's, on packed rows): out = sum_c w_c out_c / sum_c w_c with
+// w_c = exp(lse_c - max).  32 lanes read a row, KP groups of them share its chunks.
+template <bool BF16, int KP>
+__global__ __launch_bounds__(32 * (KP < 8 ? 8 : KP)) void rows_merge_kernel(RowsAttnArgs a) {
+  constexpr int kRows = KP < 8 ? 8 / KP : 1;  // rows of a workgroup
+  __shared__ float sm_m[kRows * KP], sm_l[kRows * KP];
+  __shared__ f32x4 sm_o[kRows * KP][32];
+  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5, k = group % KP;
+  const int64_t first = (int64_t)row_start(a.row_begin, 0, a.rows) * a.Hq;
+  const int64_t r = first + (int64_t)blockIdx.x * kRows + group / KP, n = (int64_t)a.rows * a.Hq;
+  const bool live = r < (int64_t)row_start(a.row_begin, a.s.B, a.rows) * a.Hq;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  if (live) {
+    for (int c0 = k; c0 < a.nc; c0 += 4 * KP) {
+      float x[4];
+      f32x4 v[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = min(c0 + u * KP, a.nc - 1);
+        x[u] = a.part_lse[c * n + r];
+        v[u] = reinterpret_cast<const f32x4*>(a.part_out + (c * n + r) * kHeadDim)[lane];
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (c0 + u * KP >= a.nc || x[u] == -INFINITY) continue;  // an empty part's row may hold anything
+        const float m_new = fmaxf(m, x[u]);
+        const float w = expf(x[u] - m_new), old = m == -INFINITY ? 0.f : expf(m - m_new);
+        l = l * old + w;
+        o = o * old + w * v[u];
+        m = m_new;
+      }
+    }
+  }
+  if (KP > 1) {
+    race_check_delay(threadIdx.x >> 6);
+    if (lane == 0) sm_m[group] = m, sm_l[group] = l;
+    sm_o[group][lane] = o;
+    __syncthreads();
+    race_check_barrier();
+    if (!live || k != 0) return;
+    float M = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < KP; ++i) M = fmaxf(M, sm_m[group + i]);
+    l = 0.f;
+    o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < KP; ++i) {
+      // A group without a live part adds nothing; one whose only parts are NaN has no maximum but NaN sums.
+      const float mi = sm_m[group + i], li = sm_l[group + i];
+      if (li == 0.f) continue;
+      const float w = mi == M ? 1.f : expf(mi - M);
+      l += w * li;
+      o += w * sm_o[group + i][lane];
+    }
+    m = M;
+  }
+  if (!live) return;
+  const bool empty = l == 0.f;
+  o *= empty ? 0.f : 1.0f / l;
+  if (BF16)
+    reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + r * kHeadDim)[lane] =
+        u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
+  else
+    reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + r * kHeadDim)[lane] = o;
+  if (a.lse != nullptr && lane == 0) a.lse[r] = empty ? -INFINITY : m + logf(l);
+}
+
+template <bool BF16>
+void launch_merge_rows(const RowsAttnArgs& a, hipStream_t stream) {
+  const int64_t n = (int64_t)a.rows * a.Hq;
+  if (a.merge_groups == 1)
+    hipLaunchKernelGGL((rows_merge_kernel<BF16, 1>), dim3((unsigned)((n + 7) / 8)), dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((rows_merge_kernel<BF16, 8>), dim3((unsigned)n), dim3(256), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_rows_attn(const RowsAttnArgs& a, RowsMode mode, bool bf16, hipStream_t stream) {
+hipError_t launch_rows_attn(const RowsAttnArgs& args, RowsMode mode, bool bf16, hipStream_t stream) {
+  RowsAttnArgs a = args;
+  a.tiles = (unsigned)((int64_t)a.rows * a.G / CT + a.s.B) * (unsigned)a.s.Hkv;
+  a.by_tiles.set(a.tiles);
+  const dim3 grid(a.tiles * (unsigned)a.nc), block(64 * W);
   if (mode == RowsMode::kTree) {
-    if (bf16) launch_wide<RowsMode::kTree, true>(a, stream);
-    else launch_wide<RowsMode::kTree, false>(a, stream);
+    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, false>), grid, block, 0, stream, a);
   } else {
-    if (bf16) launch_wide<RowsMode::kWindow, true>(a, stream);
-    else launch_wide<RowsMode::kWindow, false>(a, stream);
+    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, true>), grid, block, 0, stream, a);
+    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, false>), grid, block, 0, stream, a);
   }
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.nc == 1) return e;
+  if (bf16) launch_merge_rows<true>(a, stream);
+  else launch_merge_rows<false>(a, stream);
   return hipGetLastError();
 }
 

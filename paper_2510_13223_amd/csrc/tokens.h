@@ -35,7 +35,17 @@ struct RowsAttnArgs {
   FastDiv by_hkv, by_g;
   void* out;                 // [rows][Hq][128], fp32 or bf16
   float* lse;                // [rows][Hq] or NULL
+  // A tile's steps (32 tokens each) are cut into nc chunks of at least `least` steps, whose partial rows
+  // [nc][rows][Hq] the merge joins (nc 1: none); merge_groups (1 or 8) groups of lanes share a row's chunks.
+  int nc, least, merge_groups;
+  float* part_out;
+  float* part_lse;
+  unsigned tiles;    // workgroups of a chunk (set by the launcher)
+  FastDiv by_tiles;
 };
+
+constexpr int kRowsTile = 128;  // columns (rows x heads of a group) of a workgroup
+constexpr int kRowsStep = 32;   // tokens of a step
 
 enum class RowsMode { kTree, kWindow };
 

@@ -23,7 +23,11 @@ constexpr int kHeadDim = 128;
 constexpr int kBlockSize = 16;
 constexpr int64_t kMaxRows = int64_t{1} << 24;           // rows: a workgroup of 256 threads each in 32 bits
 constexpr int64_t kMaxHeadRows = int64_t{1} << 26;       // rows x heads
+constexpr int64_t kMaxPairs = int64_t{1} << 23;          // batch x kv heads of an attention: its workgroups likewise
 constexpr int kMaxTreeParts = 63;                        // ranges of a tree call: with the nodes, one per lane
+constexpr int64_t kMaxLaunchItems = UINT32_MAX;          // work-items of one launch
+constexpr int kMaxChunks = 128;
+constexpr int kRowsTileRows = 128;                       // rows of a tile at most (a group of 1)
 constexpr int64_t kMaxListBlocks = int64_t{1} << 30;     // blocks of all ranges of a sequence
 
 bana::CacheShape shape_of(const bana_dims* d) {
@@ -42,6 +46,7 @@ bana_status check_attention(const bana_dims* d, int64_t rows, const int32_t* row
                             const void* out, int32_t out_type, const void* workspace) {
   bana_status st = check_dims(d);
   if (st == BANA_OK) st = check_rows(d, rows, d->num_q_heads);
+  if (st == BANA_OK && (int64_t)d->batch * d->num_kv_heads > kMaxPairs) st = BANA_ERR_UNSUPPORTED;
   if (st != BANA_OK) return st;
   if (!row_begin || !q || !k_cache || !v_cache || !block_table || !out) return BANA_ERR_INVALID;
   if (out_type != BANA_OUT_F32 && out_type != BANA_OUT_BF16) return BANA_ERR_INVALID;
@@ -73,18 +78,85 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
   return a;
 }
 
+#ifndef BANA_TARGET
+#define BANA_TARGET 512
+#define BANA_LEAST 2
+#endif
+
+// Chunks of a call whose longest row sees at most `tokens` tokens.
+struct RowsPlan {
+  int nc = 1;
+  int least = 1;  // steps of a chunk at least
+  int merge_groups = 1;
+};
+
+RowsPlan plan_rows(const bana_dims* d, int64_t rows, int64_t tokens) {
+  RowsPlan p;
+  const int G = d->num_q_heads / d->num_kv_heads;
+  const int64_t tiles = std::max<int64_t>(rows * G / bana::kRowsTile, std::min<int64_t>(d->batch, rows));
+  const int64_t groups = tiles * d->num_kv_heads;
+  const int64_t steps = (tokens + bana::kRowsStep - 1) / bana::kRowsStep;
+  const int64_t mean = d->total_range_tokens > 0
+                           ? std::min<int64_t>(steps, d->total_range_tokens / d->batch / bana::kRowsStep + 1)
+                           : steps;
+  const int64_t even = mean > (int64_t{1} << 30) / groups ? mean : (mean * groups + BANA_TARGET - 1) / BANA_TARGET;
+  const int64_t chunk = std::max<int64_t>(even, BANA_LEAST);
+  p.nc = (int)std::min<int64_t>((steps + chunk - 1) / chunk, kMaxChunks);
+  p.least = (int)std::min<int64_t>(chunk, INT32_MAX);
+  if (p.nc < 1) p.nc = 1;
+  const int64_t launched = (rows * G / bana::kRowsTile + d->batch) * d->num_kv_heads;
+  if (launched * p.nc * 256 > kMaxLaunchItems) p.nc = 1;
+  p.merge_groups = rows * d->num_q_heads < 4096 && p.nc > 4 ? 8 : 1;
+  return p;
+}
+
+// Workspace: partial rows [nc][rows][Hq][128] fp32, then their lse.
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t part_bytes(const bana_dims* d, int64_t rows, const RowsPlan& p) {
+  return align256((size_t)p.nc * rows * d->num_q_heads * kHeadDim * sizeof(float));
+}
+size_t workspace_for(const bana_dims* d, int64_t rows, const RowsPlan& p) {
+  if (p.nc == 1) return 0;
+  return part_bytes(d, rows, p) + align256((size_t)p.nc * rows * d->num_q_heads * sizeof(float));
+}
+
+// The most tokens that a sequence has in the cache.
+int64_t longest(const bana_dims* d) {
+  const int64_t span = (int64_t)d->max_blocks_per_seq * kBlockSize;
+  return d->max_range_tokens > 0 ? std::min<int64_t>(span, d->max_range_tokens) : span;
+}
+int64_t window_tokens(const bana_dims* d, int32_t window, int32_t sinks) {
+  return std::min<int64_t>(longest(d), (int64_t)window + sinks + kRowsTileRows);
+}
+
+void set_plan(bana::RowsAttnArgs& a, const bana_dims* d, RowsPlan p, void* workspace, size_t workspace_bytes) {
+  if (p.nc > 1 && (workspace == nullptr || workspace_bytes < workspace_for(d, a.rows, p))) p = RowsPlan{};
+  a.nc = p.nc;
+  a.least = p.least;
+  a.merge_groups = p.merge_groups;
+  if (p.nc > 1) {
+    a.part_out = static_cast<float*>(workspace);
+    a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(d, a.rows, p));
+  }
+}
+
+bool plannable(const bana_dims* d, int64_t rows) {
+  return check_dims(d) == BANA_OK && rows > 0 && check_rows(d, rows, d->num_q_heads) == BANA_OK &&
+         (int64_t)d->batch * d->num_kv_heads <= kMaxPairs;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t bana_tree_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_t n_parts) {
-  (void)d, (void)rows, (void)n_parts;
-  return 0;
+  if (!plannable(d, rows) || n_parts < 1 || n_parts > kMaxTreeParts) return 0;
+  return workspace_for(d, rows, plan_rows(d, rows, longest(d)));
 }
 
 size_t bana_window_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_t window, int32_t sinks) {
-  (void)d, (void)rows, (void)window, (void)sinks;
-  return 0;
+  if (!plannable(d, rows) || window < 1 || sinks < 0) return 0;
+  return workspace_for(d, rows, plan_rows(d, rows, window_tokens(d, window, sinks)));
 }
 
 bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_begin, const void* q,
@@ -105,7 +177,7 @@ bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_
   a.n_parts = n_parts;
   a.tree_begin = tree_begin;
   a.mask = tree_mask;
-  (void)workspace_bytes;
+  set_plan(a, d, plan_rows(d, rows, longest(d)), workspace, workspace_bytes);
   return device_status(bana::launch_rows_attn(a, bana::RowsMode::kTree, out_type == BANA_OUT_BF16,
                                               static_cast<hipStream_t>(stream)));
 }
@@ -127,7 +199,7 @@ bana_status bana_window_attn(const bana_dims* d, int64_t rows, const int32_t* ro
   a.seq_lens = seq_lens;
   a.window = window;
   a.sinks = sinks;
-  (void)workspace_bytes;
+  set_plan(a, d, plan_rows(d, rows, window_tokens(d, window, sinks)), workspace, workspace_bytes);
   return device_status(bana::launch_rows_attn(a, bana::RowsMode::kWindow, out_type == BANA_OUT_BF16,
                                               static_cast<hipStream_t>(stream)));
 }
