@@ -251,30 +251,31 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
 // changes no relative rounding), which spares most steps the rescaling of the sums.
 constexpr int kTileBytes = kTileElems * 2;
-#ifndef BANA_RING
-#define BANA_RING 3
-#define BANA_EU (BF16 ? 3 : 2)
-#endif
-constexpr int kRing = BANA_RING;
+constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
 constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
 constexpr int kVStep = 2 * kTileBytes;
 constexpr int kStep = kKStep + kVStep;          // K, then V
 constexpr float kSlack = 8.f;
-constexpr int NT = 2, W = 4;      // column tiles of a wavefront, wavefronts
-constexpr int CT = 16 * NT * W;  // columns of a workgroup
-static_assert(CT == kRowsTile, "the planner's tile");
+constexpr int W = 4;  // wavefronts of a workgroup
+static_assert(16 * 2 * W == kRowsTile, "the planner's tile");
 
 
-// 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.
+// 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.  STREAM: read by
+// this workgroup only, past the caches.
+#define FETCH_4K(hint)                                                                                        \
+  asm volatile(                                                                                               \
+      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %5" hint                                   \
+      "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5" hint                      \
+      "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5" hint                      \
+      "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5" hint ::"v"(offset[0]),    \
+      "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(lds), "s"(base)                                     \
+      : "memory", "m0", "scc")
+template <bool STREAM>
 __device__ __forceinline__ void fetch_4k(uint64_t base, const uint32_t (&offset)[4], uint32_t lds) {
-  asm volatile(
-      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %5\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5\n\t"
-      "s_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5" ::"v"(offset[0]),
-      "v"(offset[1]), "v"(offset[2]), "v"(offset[3]), "s"(lds), "s"(base)
-      : "memory", "m0", "scc");
+  if (STREAM) FETCH_4K(" nt");
+  else FETCH_4K("");
 }
+#undef FETCH_4K
 
 struct Yes {
   static constexpr bool value = true;
@@ -283,9 +284,14 @@ struct No {
   static constexpr bool value = false;
 };
 
-template <RowsMode MODE, bool BF16>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(BANA_EU, BANA_EU)))
+template <bool BF16, int NT>
+constexpr int kWavesPerSimd = BF16 || NT == 1 ? 3 : 2;
+
+template <RowsMode MODE, bool BF16, int NT>
+__global__ __launch_bounds__(64 * W)
+__attribute__((amdgpu_waves_per_eu(kWavesPerSimd<BF16, NT>, kWavesPerSimd<BF16, NT>)))
 void rows_attn_kernel(RowsAttnArgs a) {
+  constexpr int CT = 16 * NT * W;     // columns of a workgroup
   constexpr int kLoads = 4;           // requests of a wavefront and step, 1 KiB each
   constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight
   __shared__ __attribute__((aligned(16))) char ring[kRing * kStep];
@@ -362,7 +368,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
       }
       const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(tile_hi, step & 63) << 32 |
                             (uint32_t)__builtin_amdgcn_readlane(tile_lo, step & 63);
-      fetch_4k(base, lane_off, __builtin_amdgcn_readfirstlane(ring_at + at));
+      fetch_4k<NT == 1>(base, lane_off, __builtin_amdgcn_readfirstlane(ring_at + at));
     };
 #pragma unroll
     for (int x = 0; x < kRing - 1; ++x) request(x, x * kStep);
@@ -645,6 +651,13 @@ __global__ __launch_bounds__(32 * (KP < 8 ? 8 : KP)) void rows_merge_kernel(Rows
   if (a.lse != nullptr && lane == 0) a.lse[r] = empty ? -INFINITY : m + logf(l);
 }
 
+template <RowsMode MODE, bool BF16>
+void launch_tiles(const RowsAttnArgs& a, hipStream_t stream) {
+  const dim3 grid(a.tiles * (unsigned)a.nc), block(64 * W);
+  if (a.tile == kRowsTile) hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 2>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 1>), grid, block, 0, stream, a);
+}
+
 template <bool BF16>
 void launch_merge_rows(const RowsAttnArgs& a, hipStream_t stream) {
   const int64_t n = (int64_t)a.rows * a.Hq;
@@ -658,16 +671,10 @@ void launch_merge_rows(const RowsAttnArgs& a, hipStream_t stream) {
 
 hipError_t launch_rows_attn(const RowsAttnArgs& args, RowsMode mode, bool bf16, hipStream_t stream) {
   RowsAttnArgs a = args;
-  a.tiles = (unsigned)((int64_t)a.rows * a.G / CT + a.s.B) * (unsigned)a.s.Hkv;
+  a.tiles = (unsigned)((int64_t)a.rows * a.G / a.tile + a.s.B) * (unsigned)a.s.Hkv;
   a.by_tiles.set(a.tiles);
-  const dim3 grid(a.tiles * (unsigned)a.nc), block(64 * W);
-  if (mode == RowsMode::kTree) {
-    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kTree, false>), grid, block, 0, stream, a);
-  } else {
-    if (bf16) hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, true>), grid, block, 0, stream, a);
-    else hipLaunchKernelGGL((rows_attn_kernel<RowsMode::kWindow, false>), grid, block, 0, stream, a);
-  }
+  if (mode == RowsMode::kTree) bf16 ? launch_tiles<RowsMode::kTree, true>(a, stream) : launch_tiles<RowsMode::kTree, false>(a, stream);
+  else bf16 ? launch_tiles<RowsMode::kWindow, true>(a, stream) : launch_tiles<RowsMode::kWindow, false>(a, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nc == 1) return e;
   if (bf16) launch_merge_rows<true>(a, stream);

@@ -37,6 +37,7 @@ struct RowsAttnArgs {
   float* lse;                // [rows][Hq] or NULL
   // A tile's steps (32 tokens each) are cut into nc chunks of at least `least` steps, whose partial rows
   // [nc][rows][Hq] the merge joins (nc 1: none); merge_groups (1 or 8) groups of lanes share a row's chunks.
+  int tile;  // columns (rows x heads of a group) of a workgroup: kRowsTile or half of it
   int nc, least, merge_groups;
   float* part_out;
   float* part_lse;
@@ -44,7 +45,7 @@ struct RowsAttnArgs {
   FastDiv by_tiles;
 };
 
-constexpr int kRowsTile = 128;  // columns (rows x heads of a group) of a workgroup
+constexpr int kRowsTile = 128;  // columns of a workgroup, half as many where sequences have few
 constexpr int kRowsStep = 32;   // tokens of a step
 
 enum class RowsMode { kTree, kWindow };

@@ -27,6 +27,11 @@ constexpr int64_t kMaxPairs = int64_t{1} << 23;          // batch x kv heads of 
 constexpr int kMaxTreeParts = 63;                        // ranges of a tree call: with the nodes, one per lane
 constexpr int64_t kMaxLaunchItems = UINT32_MAX;          // work-items of one launch
 constexpr int kMaxChunks = 128;
+constexpr int kMinChunkSteps = 2;
+constexpr double kStepLatencyUs = 0.7;                   // of the planner's estimate (plan_rows)
+constexpr double kStartSteps = 1.5;                      // a workgroup's start, in steps
+constexpr double kMergeUs = 4;
+constexpr double kPartBytesPerUs = 4e6;
 constexpr int kRowsTileRows = 128;                       // rows of a tile at most (a group of 1)
 constexpr int64_t kMaxListBlocks = int64_t{1} << 30;     // blocks of all ranges of a sequence
 
@@ -78,33 +83,57 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
   return a;
 }
 
-#ifndef BANA_TARGET
-#define BANA_TARGET 512
-#define BANA_LEAST 2
-#endif
-
-// Chunks of a call whose longest row sees at most `tokens` tokens.
+// How a call's tiles are cut.  A tile is 128 columns (rows x heads of a group), or 64 where sequences have no more
+// on the mean: four wavefronts of 16 columns then share what two of 32 would do one after the other (24 drafts of
+// 13 nodes, groups of 4, fp32: 108 -> 80 us), and the loads go past the caches, as no other tile reads them.
+//
+// A tile's list of steps (32 tokens) is cut into chunks where that is estimated to be faster.  With n
+// workgroups at work, of at most `slots`, a step takes max(latency, n x kStepNs): alone it is bound by the chain of
+// its products, all together by HBM or the matrix and vector units.  Each workgroup's start costs it
+// kStartSteps more; the last chunks run on while the GPU empties, a quarter of a chunk's latency on the mean; each chunk's partial rows are written and read once more, after a
+// launch.  Times in us, measured on MI355X (kStepNs: the whole call's time per step, ns):
+//   64 columns, bf16 / fp32:  2.5 / 2.7     128 columns, bf16 / fp32:  2.2 / 4.4     latency of a step 0.7
+// Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.8; 64 rows, window 4096, 202
+// -> 173; 2048 rows x 64 heads, 3200 to 12800 tokens, 656 -> 629; prompts of 750 rows, window 512, stay whole (58,
+// in two chunks 89).
 struct RowsPlan {
   int nc = 1;
   int least = 1;  // steps of a chunk at least
   int merge_groups = 1;
+  int tile = bana::kRowsTile;
 };
 
-RowsPlan plan_rows(const bana_dims* d, int64_t rows, int64_t tokens) {
+// The call's longest row sees at most `tokens` tokens.
+RowsPlan plan_rows(const bana_dims* d, int64_t rows, int64_t tokens, bool bf16) {
   RowsPlan p;
   const int G = d->num_q_heads / d->num_kv_heads;
-  const int64_t tiles = std::max<int64_t>(rows * G / bana::kRowsTile, std::min<int64_t>(d->batch, rows));
-  const int64_t groups = tiles * d->num_kv_heads;
-  const int64_t steps = (tokens + bana::kRowsStep - 1) / bana::kRowsStep;
+  const bool thin = rows * G <= (int64_t)d->batch * (bana::kRowsTile / 2);
+  p.tile = thin ? bana::kRowsTile / 2 : bana::kRowsTile;
+  const int64_t tiles = std::max<int64_t>(rows * G / p.tile, std::min<int64_t>(d->batch, rows));
+  const double groups = (double)tiles * d->num_kv_heads;
+  const int64_t steps = std::max<int64_t>(1, (tokens + bana::kRowsStep - 1) / bana::kRowsStep);
   const int64_t mean = d->total_range_tokens > 0
                            ? std::min<int64_t>(steps, d->total_range_tokens / d->batch / bana::kRowsStep + 1)
                            : steps;
-  const int64_t even = mean > (int64_t{1} << 30) / groups ? mean : (mean * groups + BANA_TARGET - 1) / BANA_TARGET;
-  const int64_t chunk = std::max<int64_t>(even, BANA_LEAST);
-  p.nc = (int)std::min<int64_t>((steps + chunk - 1) / chunk, kMaxChunks);
-  p.least = (int)std::min<int64_t>(chunk, INT32_MAX);
-  if (p.nc < 1) p.nc = 1;
-  const int64_t launched = (rows * G / bana::kRowsTile + d->batch) * d->num_kv_heads;
+  const double slots = bf16 || thin ? 768 : 512;
+  const double step_us = (thin ? (bf16 ? 2.5 : 2.7) : bf16 ? 2.2 : 4.4) * 1e-3;
+  const double part_us = (double)rows * d->num_q_heads * 2 * (kHeadDim + 1) * sizeof(float) / kPartBytesPerUs;
+  double best = 0;
+  for (int nc = 1; nc <= kMaxChunks; ++nc) {
+    const int64_t chunk = (steps + nc - 1) / nc;
+    if (nc > 1 && chunk < kMinChunkSteps) break;
+    const double used = mean < steps ? std::min<double>(nc, (double)mean / chunk + 0.5) : nc;  // chunks of a tile
+    const double busy = std::min(slots, std::max(groups * used, 1.0));
+    const double one = (chunk + kStartSteps) * std::max(kStepLatencyUs, step_us * busy);
+    const double all = groups * (mean + used * kStartSteps) * step_us + 0.25 * chunk * kStepLatencyUs;
+    const double time = std::max(one, all) + (nc > 1 ? kMergeUs + used * part_us : 0);
+    if (nc == 1 || time < best) {
+      best = time;
+      p.nc = nc;
+      p.least = (int)std::min<int64_t>(chunk, INT32_MAX);
+    }
+  }
+  const int64_t launched = (rows * G / p.tile + d->batch) * d->num_kv_heads;
   if (launched * p.nc * 256 > kMaxLaunchItems) p.nc = 1;
   p.merge_groups = rows * d->num_q_heads < 4096 && p.nc > 4 ? 8 : 1;
   return p;
@@ -130,7 +159,8 @@ int64_t window_tokens(const bana_dims* d, int32_t window, int32_t sinks) {
 }
 
 void set_plan(bana::RowsAttnArgs& a, const bana_dims* d, RowsPlan p, void* workspace, size_t workspace_bytes) {
-  if (p.nc > 1 && (workspace == nullptr || workspace_bytes < workspace_for(d, a.rows, p))) p = RowsPlan{};
+  if (p.nc > 1 && (workspace == nullptr || workspace_bytes < workspace_for(d, a.rows, p))) p.nc = p.least = 1;
+  a.tile = p.tile;
   a.nc = p.nc;
   a.least = p.least;
   a.merge_groups = p.merge_groups;
@@ -138,6 +168,12 @@ void set_plan(bana::RowsAttnArgs& a, const bana_dims* d, RowsPlan p, void* works
     a.part_out = static_cast<float*>(workspace);
     a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(d, a.rows, p));
   }
+}
+
+// The workspace of a call with either type of result.
+size_t most_workspace(const bana_dims* d, int64_t rows, int64_t tokens) {
+  return std::max(workspace_for(d, rows, plan_rows(d, rows, tokens, true)),
+                  workspace_for(d, rows, plan_rows(d, rows, tokens, false)));
 }
 
 bool plannable(const bana_dims* d, int64_t rows) {
@@ -151,12 +187,12 @@ extern "C" {
 
 size_t bana_tree_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_t n_parts) {
   if (!plannable(d, rows) || n_parts < 1 || n_parts > kMaxTreeParts) return 0;
-  return workspace_for(d, rows, plan_rows(d, rows, longest(d)));
+  return most_workspace(d, rows, longest(d));
 }
 
 size_t bana_window_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_t window, int32_t sinks) {
   if (!plannable(d, rows) || window < 1 || sinks < 0) return 0;
-  return workspace_for(d, rows, plan_rows(d, rows, window_tokens(d, window, sinks)));
+  return most_workspace(d, rows, window_tokens(d, window, sinks));
 }
 
 bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_begin, const void* q,
@@ -177,7 +213,7 @@ bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_
   a.n_parts = n_parts;
   a.tree_begin = tree_begin;
   a.mask = tree_mask;
-  set_plan(a, d, plan_rows(d, rows, longest(d)), workspace, workspace_bytes);
+  set_plan(a, d, plan_rows(d, rows, longest(d), out_type == BANA_OUT_BF16), workspace, workspace_bytes);
   return device_status(bana::launch_rows_attn(a, bana::RowsMode::kTree, out_type == BANA_OUT_BF16,
                                               static_cast<hipStream_t>(stream)));
 }
@@ -199,7 +235,7 @@ bana_status bana_window_attn(const bana_dims* d, int64_t rows, const int32_t* ro
   a.seq_lens = seq_lens;
   a.window = window;
   a.sinks = sinks;
-  set_plan(a, d, plan_rows(d, rows, window_tokens(d, window, sinks)), workspace, workspace_bytes);
+  set_plan(a, d, plan_rows(d, rows, window_tokens(d, window, sinks), out_type == BANA_OUT_BF16), workspace, workspace_bytes);
   return device_status(bana::launch_rows_attn(a, bana::RowsMode::kWindow, out_type == BANA_OUT_BF16,
                                               static_cast<hipStream_t>(stream)));
 }

@@ -53,7 +53,8 @@ hipError_t launch_rows_attn(const RowsAttnArgs& a, RowsMode mode, bool bf16, hip
   const unsigned __int128 head_rows = (unsigned __int128)a.rows * a.Hq;
   REQUIRE(inside(a.q, head_rows * 256) && inside(a.row_begin, ((unsigned __int128)a.s.B + 1) * 4));
   REQUIRE(inside(a.out, head_rows * 128 * (bf16 ? 2 : 4)) && (a.lse == nullptr || inside(a.lse, head_rows * 4)));
-  const uint64_t groups = ((uint64_t)a.rows * a.G / kRowsTile + a.s.B) * a.s.Hkv;
+  REQUIRE(a.tile == kRowsTile || a.tile == kRowsTile / 2);
+  const uint64_t groups = ((uint64_t)a.rows * a.G / a.tile + a.s.B) * a.s.Hkv;
   REQUIRE(a.nc >= 1 && a.least >= 1 && groups * a.nc * 256 <= UINT32_MAX);
   REQUIRE(a.merge_groups == 1 || a.merge_groups == 8);
   if (a.nc > 1) {
