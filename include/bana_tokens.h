@@ -86,6 +86,7 @@ size_t bana_window_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_
  * Keys and values of new tokens into the cache: row row_begin[b] + i becomes token first_token[b] + i of
  * sequence b, bit for bit.  Rows whose token lies outside the table, or whose table entry names no block of the pool,
  * are skipped.  Two rows of one call must not name the same slot.  Of d, num_q_heads is not used.
+ * BANA_ERR_UNSUPPORTED: rows as above, batch * num_kv_heads above 2^18.
  *   k_rows, v_rows  bf16 [rows][num_kv_heads][128]
  */
 bana_status bana_append_kv(const bana_dims* d, int64_t rows, const int32_t* row_begin, const int32_t* first_token,
@@ -97,7 +98,8 @@ bana_status bana_append_kv(const bana_dims* d, int64_t rows, const int32_t* row_
  * first_token[b] + kept[b][i] was, i < n_kept[b], bit for bit.  kept[b] increases strictly from
  * kept[b][0] >= 0 on (an accepted path among drafted tokens, or what an eviction leaves of a sequence).
  * The tokens behind the last one moved keep what they held.  The blocks written must belong to one
- * sequence only.  Tokens outside the table or in no block of the pool are skipped.
+ * sequence only.  Tokens outside the table or in no block of the pool are skipped.  BANA_ERR_UNSUPPORTED:
+ * batch * num_kv_heads above 2^18.
  *   kept    int32 [batch][max_kept]
  *   n_kept  int32 [batch], clamped to [0, max_kept]
  */
@@ -128,7 +130,8 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
  * (clamped to the table's span).  One source may have several destinations.
  * bana_release_kv_blocks: for every sequence the entries from ceil(keep_lens[b] / 16) on are given back:
  * count - 1, entry -1 (keep_lens[b] <= 0: all of them; beyond the table: none).
- * Of d, num_q_heads is not used; nor are the heads in reserve and release.
+ * Of d, num_q_heads is not used; nor are the heads in reserve and release.  BANA_ERR_UNSUPPORTED: num_blocks above
+ * 2^31 - 1, n of 2^20 or more.
  */
 bana_status bana_reserve_kv_blocks(const bana_dims* d, int32_t* block_table, const int32_t* seq_lens,
                                    const int32_t* need_lens, int32_t* block_refs, int32_t* status, void* workspace,

@@ -24,6 +24,8 @@ constexpr int kBlockSize = 16;
 constexpr int64_t kMaxRows = int64_t{1} << 24;           // rows: a workgroup of 256 threads each in 32 bits
 constexpr int64_t kMaxHeadRows = int64_t{1} << 26;       // rows x heads
 constexpr int64_t kMaxPairs = int64_t{1} << 23;          // batch x kv heads of an attention: its workgroups likewise
+constexpr int64_t kMaxTokenPairs = int64_t{1} << 18;     // of append and compact: 32 workgroups each in 32 bits
+constexpr int kMaxForks = 1 << 20;                       // 8 workgroups each in 32 bits
 constexpr int kMaxTreeParts = 63;                        // ranges of a tree call: with the nodes, one per lane
 constexpr int64_t kMaxLaunchItems = UINT32_MAX;          // work-items of one launch
 constexpr int kMaxChunks = 128;
@@ -245,6 +247,7 @@ bana_status bana_append_kv(const bana_dims* d, int64_t rows, const int32_t* row_
                            void* v_cache, void* stream) {
   bana_status st = check_dims(d);
   if (st == BANA_OK) st = check_rows(d, rows, d->num_kv_heads);
+  if (st == BANA_OK && (int64_t)d->batch * d->num_kv_heads > kMaxTokenPairs) st = BANA_ERR_UNSUPPORTED;
   if (st != BANA_OK) return st;
   if (!row_begin || !first_token || !k_rows || !v_rows || !block_table || !k_cache || !v_cache)
     return BANA_ERR_INVALID;
@@ -262,8 +265,7 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
   if (!k_cache || !v_cache || !block_table || !first_token || !kept || !n_kept || max_kept < 0)
     return BANA_ERR_INVALID;
   if (!aligned16(k_cache) || !aligned16(v_cache)) return BANA_ERR_INVALID;
-  // A workgroup of 256 threads per (sequence, kv head) in 32 bits.
-  if ((int64_t)d->batch * d->num_kv_heads >= kMaxRows) return BANA_ERR_UNSUPPORTED;
+  if ((int64_t)d->batch * d->num_kv_heads > kMaxTokenPairs) return BANA_ERR_UNSUPPORTED;
   if (max_kept == 0) return BANA_OK;
   return device_status(bana::launch_compact(k_cache, v_cache, block_table, first_token, kept, max_kept, n_kept,
                                             shape_of(d), static_cast<hipStream_t>(stream)));
@@ -280,7 +282,7 @@ bana_status bana_reserve_kv_blocks(const bana_dims* d, int32_t* block_table, con
   const bana_status st = check_dims(d);
   if (st != BANA_OK) return st;
   if (!block_table || !seq_lens || !need_lens || !block_refs || !status || !workspace || !aligned16(workspace) ||
-      workspace_bytes < bana_kv_blocks_workspace_bytes(d))
+      !aligned16(block_refs) || workspace_bytes < bana_kv_blocks_workspace_bytes(d))
     return BANA_ERR_INVALID;
   if (d->num_blocks > INT32_MAX) return BANA_ERR_UNSUPPORTED;  // table entries are 32-bit
   return device_status(bana::launch_reserve(block_table, seq_lens, need_lens, block_refs, d->num_blocks, status,
@@ -296,9 +298,9 @@ bana_status bana_fork_kv_seqs(const bana_dims* d, const int32_t* src_seq, const 
   if (st != BANA_OK) return st;
   if (!src_seq || !dst_seq || n < 0 || n > d->batch || !k_cache || !v_cache || !block_table || !seq_lens ||
       !block_refs || !status || !workspace || !aligned16(workspace) || !aligned16(k_cache) || !aligned16(v_cache) ||
-      workspace_bytes < bana_kv_blocks_workspace_bytes(d))
+      !aligned16(block_refs) || workspace_bytes < bana_kv_blocks_workspace_bytes(d))
     return BANA_ERR_INVALID;
-  if (d->num_blocks > INT32_MAX || n >= kMaxRows) return BANA_ERR_UNSUPPORTED;
+  if (d->num_blocks > INT32_MAX || n >= kMaxForks) return BANA_ERR_UNSUPPORTED;
   if (n == 0) return BANA_OK;
   return device_status(bana::launch_fork(src_seq, dst_seq, n, k_cache, v_cache, block_table, seq_lens, block_refs,
                                          d->num_blocks, status, static_cast<int32_t*>(workspace), shape_of(d),

@@ -78,7 +78,7 @@ hipError_t launch_append(const void* k_rows, const void* v_rows, int rows, const
                          const int32_t* first, const int32_t* table, void* k, void* v, CacheShape s, hipStream_t) {
   ++g_launches;
   check_shape(s, table);
-  REQUIRE(rows >= 1 && (uint64_t)rows * 256 <= UINT32_MAX);
+  REQUIRE(rows >= 1 && ((uint64_t)rows / 16 + 2 * (uint64_t)s.B) * s.Hkv * 256 <= UINT32_MAX);
   const unsigned __int128 bytes = (unsigned __int128)rows * s.Hkv * 256;
   REQUIRE(inside(k_rows, bytes) && inside(v_rows, bytes) && inside(k, 1) && inside(v, 1));
   REQUIRE(inside(row_begin, ((unsigned __int128)s.B + 1) * 4) && inside(first, (unsigned __int128)s.B * 4));
@@ -89,7 +89,7 @@ hipError_t launch_compact(void* k, void* v, const int32_t* table, const int32_t*
                           int max_kept, const int32_t* n_kept, CacheShape s, hipStream_t) {
   ++g_launches;
   check_shape(s, table);
-  REQUIRE(max_kept >= 1 && (uint64_t)s.B * s.Hkv * 256 <= UINT32_MAX && inside(k, 1) && inside(v, 1));
+  REQUIRE(max_kept >= 1 && (uint64_t)s.B * s.Hkv * 32 * 256 <= UINT32_MAX && inside(k, 1) && inside(v, 1));
   REQUIRE(inside(first, (unsigned __int128)s.B * 4) && inside(n_kept, (unsigned __int128)s.B * 4));
   REQUIRE(inside(kept, (unsigned __int128)s.B * max_kept * 4));
   return hipSuccess;
@@ -114,7 +114,7 @@ hipError_t launch_reserve(int32_t* table, const int32_t* lens, const int32_t* ne
 hipError_t launch_fork(const int32_t* src, const int32_t* dst, int n, void* k, void* v, int32_t* table, int32_t* lens,
                        int32_t* refs, int64_t num_blocks, int32_t* status, int32_t* ws, CacheShape s, hipStream_t) {
   check_blocks(table, refs, num_blocks, status, ws, s);
-  REQUIRE(ws && n >= 1 && n <= s.B && (uint64_t)n * 256 <= UINT32_MAX && inside(k, 1) && inside(v, 1));
+  REQUIRE(ws && n >= 1 && n <= s.B && (uint64_t)n * 8 * 256 <= UINT32_MAX && inside(k, 1) && inside(v, 1));
   REQUIRE(inside(src, (uint64_t)n * 4) && inside(dst, (uint64_t)n * 4) && inside(lens, (unsigned __int128)s.B * 4));
   return hipSuccess;
 }

@@ -56,6 +56,8 @@ def test_append_skips_tokens_without_a_block():
 @pytest.mark.parametrize("hkv,lens,first,keep", [
     (1, [20], [0], 0.5), (8, [100, 33], [40, 17], 0.3), (2, [500, 0, 31], [0, 0, 15], 0.9), (3, [77] * 5, [13] * 5, 0.1),
     (40, [64], [0], 1.0), (2, [64, 64], [1, 30], 0.0), (4, [3000, 1], [5, 0], 0.6),
+    (1, [9000, 700], [13, 1], 0.03), (2, [2111, 0, 640, 90], [3, 0, 8, 0], 0.97), (1, [300], [7], 0.25),
+    (1, [1100, 1100], [0, 7], 1.0),
 ])
 def test_compact(hkv, lens, first, keep):
     rng = random.Random(7)
@@ -70,14 +72,19 @@ def test_compact(hkv, lens, first, keep):
     assert same(k, cache.k) and same(v, cache.v)
 
 
-def test_compact_stays_inside_whatever_the_numbers():
-    """Counts past the list, places past the table, entries of no block: skipped."""
+@pytest.mark.parametrize("behind", [0, 100])
+def test_compact_stays_inside_whatever_the_numbers(behind):
+    """Counts past the list, places past the table, entries of no block: skipped, by both kernels (a longer list)."""
     cache = tc.Cache([60, 40], 2, 8, width=5)
     cache.table[0, 2] = -1
-    kept = torch.tensor([[0, 3, 35, 50, 70, 10 ** 9], [1, 2, 3, 4, 5, 6]], dtype=torch.int32)
+    kept = torch.tensor([[0, 3, 35, 50, 70, 10 ** 9] + [10 ** 9 + 1 + i for i in range(behind)],
+                         [1, 2, 3, 4, 5, 6] + [7 + i for i in range(behind)]], dtype=torch.int32)
     k, v = cache.k.to(DEV), cache.v.to(DEV)
-    tc.compact(cache.k, cache.v, cache.table, [4, 37], kept, [9, -1])
-    bana.bana_compact_kv_tokens(k, v, cache.table.to(DEV), ints([4, 37]), kept.to(DEV), ints([9, -1]))
+    tc.compact(cache.k, cache.v, cache.table, [4, 37], kept, [900, -1])
+    bana.bana_compact_kv_tokens(k, v, cache.table.to(DEV), ints([4, 37]), kept.to(DEV), ints([900, -1]))
+    assert same(k, cache.k) and same(v, cache.v)
+    tc.compact(cache.k, cache.v, cache.table, [-3, 37], kept, [4, 6 + behind])
+    bana.bana_compact_kv_tokens(k, v, cache.table.to(DEV), ints([-3, 37]), kept.to(DEV), ints([4, 6 + behind]))
     assert same(k, cache.k) and same(v, cache.v)
 
 
