@@ -14,8 +14,8 @@
  * these calls read the shapes and, as hints for the attention, max_range_tokens (the most cached
  * tokens of a sequence, new ones included) and total_range_tokens (their sum over sequences); the other
  * hints must be valid and are ignored.  Values that live on the device are not checked on the host,
- * but no value makes a call read or write outside the buffers it was given: offsets outside the rows, the table or the
- * pool are clamped or skipped.  A wrong value gives wrong results, not a fault.
+ * but no value makes a call read or write outside the buffers it was given: offsets outside the rows, the
+ * table or the pool are clamped or skipped.  A wrong value gives wrong results, not a fault.
  *
  * Packed rows.  The new tokens of a batch are rows of dense arrays: sequence b has the rows
  * [row_begin[b], row_begin[b + 1]), n_b of them (possibly none); row_begin is int32 [batch + 1] and
@@ -42,10 +42,12 @@ extern "C" {
  * counts twice), and node j < min(n_b, 64) where bit j of tree_mask[r] is set:
  *   out[r][h] = sum_t exp(scale q[r][h].k_t - lse) v_t,   lse[r][h] = ln sum_t exp(scale q[r][h].k_t)
  * A row that sees nothing gives out = 0, lse = -inf.  tree_begin[b] < 0: the nodes are not in
- * this call's cache (another partition has them), rows see the ranges only.  Scores and sums are fp32; with an fp32 result
- * the weights enter the product with the values to 24 bits, with a bf16 result rounded to bf16.  The fp32 result and lse of several calls over
- * disjoint tokens merge exactly with bana_merge_partials (batch = rows).  A NaN among a row's scores makes the row NaN;
- * values that a row does not see never reach it, whatever they hold.
+ * this call's cache (another partition has them), rows see the ranges only.  Scores and sums are fp32; with
+ * an fp32 result the weights enter the product with the values to 24 bits, with a bf16 result rounded to
+ * bf16.  The fp32 result and lse of several calls over disjoint tokens merge exactly with
+ * bana_merge_partials (batch = rows).  A NaN among a row's scores makes the row NaN; a row whose scores are
+ * all -inf gives 0 and -inf as one that sees nothing does.  Values that a row does not see never reach it,
+ * whatever they hold.
  *   q           bf16 [rows][num_q_heads][128]
  *   kv_range_*  int32 [n_parts][batch], 1 <= n_parts <= 63
  *   tree_begin  int32 [batch]
@@ -53,11 +55,11 @@ extern "C" {
  *   out         fp32 or bf16 (out_type) [rows][num_q_heads][128]
  *   lse         fp32 [rows][num_q_heads], or NULL
  *   scale       > 0, finite
- * workspace: optional, bana_tree_attn_workspace_bytes bytes let the library split long
- * ranges over workgroups (with less the call runs unsplit, the same result up to rounding).  Calls that may overlap must not
- * share one; its contents need no initialisation.  Results are bit-identical run to run for the same
- * inputs and dims.  BANA_ERR_UNSUPPORTED: rows of 2^24 or rows * num_q_heads
- * of 2^26 or more, batch * num_kv_heads above 2^23, n_parts above 63, n_parts * max_blocks_per_seq above 2^30.
+ * workspace: optional, bana_tree_attn_workspace_bytes bytes let the library split long ranges over
+ * workgroups (with less the call runs unsplit, the same result up to rounding).  Calls that may overlap must
+ * not share one; its contents need no initialisation.  Results are bit-identical run to run for the same
+ * inputs and dims.  BANA_ERR_UNSUPPORTED: rows of 2^24 or rows * num_q_heads of 2^26 or more,
+ * batch * num_kv_heads above 2^23, n_parts above 63, n_parts * max_blocks_per_seq above 2^30.
  */
 bana_status bana_tree_attn(const bana_dims* d, int64_t rows, const int32_t* row_begin, const void* q,
                            const void* k_cache, const void* v_cache, const int32_t* block_table,
@@ -71,7 +73,8 @@ size_t bana_tree_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_t 
  * and values of the new tokens are in the cache; seq_lens[b] counts them.  Row r = row_begin[b] + i is
  * the token at position pos = seq_lens[b] - n_b + i and sees the tokens t <= pos with pos - t < window or
  * t < sinks, of these the ones in [kv_range_begin[b], kv_range_end[b]) where those are given
- * (both or neither NULL; int32 [batch]: the tokens of one partition, merged as above).  A row at a negative position sees nothing.
+ * (both or neither NULL; int32 [batch]: the tokens of one partition, merged as above).  A row at a negative
+ * position sees nothing.
  * window >= 1 (INT32_MAX: no window, plain causal attention), sinks >= 0.  n_b may be 1 (a decode step),
  * seq_lens[b] (a whole prompt) or anything between.  Everything else as for bana_tree_attn.
  */
@@ -125,13 +128,14 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
  * ceil(need_lens[b] / 16)) that are -1 receive the free blocks of the lowest numbers, in the order of
  * (b, j); their counts become 1.
  * bana_fork_kv_seqs: for i < n, sequence dst_seq[i], which has no block, becomes a copy of sequence
- * src_seq[i]: its whole blocks are shared (counts + 1), a last block that is only partly filled is copied into the free block of
- * the lowest number left, in the order of i (count 1), seq_lens[dst_seq[i]] = seq_lens[src_seq[i]]
- * (clamped to the table's span).  One source may have several destinations.
+ * src_seq[i]: its whole blocks are shared (counts + 1), a last block that is only partly filled is copied
+ * into the free block of the lowest number left, in the order of i (count 1),
+ * seq_lens[dst_seq[i]] = seq_lens[src_seq[i]] (clamped to the table's span).  One source may have several
+ * destinations.
  * bana_release_kv_blocks: for every sequence the entries from ceil(keep_lens[b] / 16) on are given back:
  * count - 1, entry -1 (keep_lens[b] <= 0: all of them; beyond the table: none).
- * Of d, num_q_heads is not used; nor are the heads in reserve and release.  BANA_ERR_UNSUPPORTED: num_blocks above
- * 2^31 - 1, n of 2^20 or more.
+ * Of d, num_q_heads is not used; nor are the heads in reserve and release.  BANA_ERR_UNSUPPORTED:
+ * num_blocks above 2^31 - 1, n of 2^20 or more, in reserve a table of 2^31 entries or more.
  */
 bana_status bana_reserve_kv_blocks(const bana_dims* d, int32_t* block_table, const int32_t* seq_lens,
                                    const int32_t* need_lens, int32_t* block_refs, int32_t* status, void* workspace,

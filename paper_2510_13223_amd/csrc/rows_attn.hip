@@ -26,10 +26,10 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kDimTiles = kHeadDim / 16;
 constexpr float kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -216,40 +216,51 @@ __device__ __forceinline__ Sight<MODE> sight_of(const RowsAttnArgs& a, const Til
   return s;
 }
 
-// Rows of one 16-column tile: lane (col, quad) has dims 16 dt + 4 quad + [0, 4).  m in powers of two.
-template <bool BF16>
+// One row: this lane has the dims STRIDE j + first + [0, 4) in acc[j].  m in powers of two.
+template <bool BF16, int STRIDE>
 __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restrict__ lse, int64_t row,
-                                          const f32x4 (&acc)[kDimTiles], float l, float m, int quad) {
+                                          const f32x4 (&acc)[kHeadDim / STRIDE], float l, float m, int first) {
   const bool empty = l == 0.f;
   const float inv = empty ? 0.f : 1.0f / l;
 #pragma unroll
-  for (int dt = 0; dt < kDimTiles; ++dt) {
-    const f32x4 o = acc[dt] * inv;
-    const int64_t at = row * kHeadDim + 16 * dt + 4 * quad;
+  for (int j = 0; j < kHeadDim / STRIDE; ++j) {
+    const f32x4 o = acc[j] * inv;
+    const int64_t at = row * kHeadDim + STRIDE * j + first;
     if (BF16)
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};
     else
       *reinterpret_cast<f32x4*>(static_cast<float*>(out) + at) = o;
   }
-  if (lse != nullptr && quad == 0) lse[row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
+  if (lse != nullptr && first == 0) lse[row] = empty ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---- the kernel: K and V shared through LDS ---------------------------------------------------------
 //
-// Four wavefronts of 32 columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
-// step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two to three
-// steps ahead) and feed the operands of all four:
-//   scores  S^T[16 tok x 16 col] twice per column tile: 4 x v_mfma_f32_16x16x32_bf16 over the 128 dims
-//   values  O^T[16 dim x 16 col] += V^T[16 dim x 32 tok] P^T[32 tok x 16 col]
-// Lane quad q of the value product takes 8 consecutive tokens: slots 8 (q & 1) + [0, 8) of block q >> 1.  The
-// rows of the two score products are assigned to tokens so that they leave exactly these 8 in that quad (row
-// 4 q + i of product x: slot 8 (q & 1) + 4 x + i of block q >> 1), so P never leaves its lane.
-// A fragment is read with one 16-byte read per lane, no two lanes on the same bank: the second block's K tile
-// lies 64 bytes off (its rows fall between the first block's); of V, each 16 dims hold the first 8 tokens of
-// all dims, then the last 8.
+// Four wavefronts of COLS columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
+// step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two steps ahead)
+// and feed the operands of all four.  A wavefront's products, for 32 columns (16: in brackets):
+//   scores  S^T[32 tok x 32 col]: 8 x v_mfma_f32_32x32x16_bf16 over the 128 dims
+//           [two of 16 tok x 16 col: 4 x v_mfma_f32_16x16x32_bf16 each]
+//   values  O^T[128 dim x 32 col] += V^T P^T: 4 tiles of 32 dims, one product of 16 tokens per block
+//           [8 tiles of 16 dims, one product of the 32 tokens]
+// A value product takes 8 consecutive tokens from each lane: slots 8 (hi & 1) + [0, 8) of a block, hi = lane / COLS.
+// The rows of the score products are assigned to tokens so that they leave exactly these in that lane, and P
+// never leaves it.  Every fragment is one 16-byte LDS read per lane, no two lanes of a phase on the same bank:
+// the second block's K tile lies 64 bytes off (16 columns read both blocks at once); of V, each 16 dims hold the
+// first 8 tokens of all dims, then the last 8.
 //
 // The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
-// changes no relative rounding), which spares most steps the rescaling of the sums.
+// changes no relative rounding), which spares most steps the rescaling of the sums.  A bf16 result takes its weights
+// rounded to bf16, half a step of the result's own type; an fp32 result takes them as three bf16 terms, 24 bits.
+// Their sum is of the unrounded ones in both.
+//
+// What bounds it, 32 columns: 16 matrix instructions of 32 cycles a step and wavefront, some 80 vector
+// instructions and 16 exponentials, 16 KiB of LDS reads; three workgroups on a CU overlap them, in part.  2 x 4096 new
+// tokens, 32 heads, window 4096, bf16: 545 us, 1.03 PFLOP/s, where a library product of 8192^3 reaches 1.47; without
+// the weights' computation 444, without the LDS reads 498, without both 401.  32 trees of 64 nodes over 8000 tokens,
+// 64 heads: 625 us.  Instructions of 16 x 16 x 32 for 32 columns: 543, 640; 64 columns a wavefront, one per
+// SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
+// 16 columns: HBM.  64 single tokens, window 4096: 176 us, 6.1 TB/s.
 constexpr int kTileBytes = kTileElems * 2;
 constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
 constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
@@ -257,11 +268,11 @@ constexpr int kVStep = 2 * kTileBytes;
 constexpr int kStep = kKStep + kVStep;          // K, then V
 constexpr float kSlack = 8.f;
 constexpr int W = 4;  // wavefronts of a workgroup
-static_assert(16 * 2 * W == kRowsTile, "the planner's tile");
-
+static_assert(32 * W == kRowsTile, "the planner's tile");
 
 // 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.  STREAM: read by
 // this workgroup only, past the caches.
+#pragma clang diagnostic ignored "-Winline-asm"  // m0 as a clobber: nothing else here uses it
 #define FETCH_4K(hint)                                                                                        \
   asm volatile(                                                                                               \
       "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %5" hint                                   \
@@ -284,19 +295,26 @@ struct No {
   static constexpr bool value = false;
 };
 
-template <bool BF16, int NT>
-constexpr int kWavesPerSimd = BF16 || NT == 1 ? 3 : 2;
+// Workgroups on a CU: the rings of three fill its LDS.  The three terms of 32 columns' weights take too many registers.
+template <bool BF16, int COLS>
+constexpr int kWavesPerSimd = BF16 || COLS == 16 ? 3 : 2;
 
-template <RowsMode MODE, bool BF16, int NT>
+template <RowsMode MODE, bool BF16, int COLS>
 __global__ __launch_bounds__(64 * W)
-__attribute__((amdgpu_waves_per_eu(kWavesPerSimd<BF16, NT>, kWavesPerSimd<BF16, NT>)))
+__attribute__((amdgpu_waves_per_eu(kWavesPerSimd<BF16, COLS>, kWavesPerSimd<BF16, COLS>)))
 void rows_attn_kernel(RowsAttnArgs a) {
-  constexpr int CT = 16 * NT * W;     // columns of a workgroup
-  constexpr int kLoads = 4;           // requests of a wavefront and step, 1 KiB each
+  constexpr bool kWide = COLS == 32;
+  constexpr int CT = COLS * W;          // columns of a workgroup
+  constexpr int kLoads = 4;             // requests of a wavefront and step, 1 KiB each
   constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight
+  constexpr int kTok = COLS / 2;        // tokens of a lane and step
+  constexpr int kGroups = kTok / 8;     // of 8, an operand of the value product each
+  constexpr int kStride = kWide ? 8 : 16;  // this lane's sums: dims kStride j + 4 hi + [0, 4)
+  constexpr int kAcc = kHeadDim / kStride;
+  constexpr int kQ = kWide ? 8 : 4;
   __shared__ __attribute__((aligned(16))) char ring[kRing * kStep];
   __shared__ int odd_tile[2];  // a V tile had values that are not finite
-  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int lane = threadIdx.x & 63, col = lane & (COLS - 1), hi = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned chunk = a.by_tiles.quotient(blockIdx.x);
   const Tile t = find_tile<CT>(a, blockIdx.x - chunk * a.tiles, lane);
@@ -308,28 +326,18 @@ void rows_attn_kernel(RowsAttnArgs a) {
   const int per = max((int)(((unsigned)steps + a.nc - 1) / (unsigned)a.nc), a.least);
   const int s0 = min((int)chunk * per, steps), np = min(per, steps - s0);
 
-  // This wavefront's columns.
-  const int cw = t.c0 + wave * 16 * NT;
-  const bool active = cw < C;
-  int64_t row[NT];
-  bool live[NT];
-  Sight<MODE> sight[NT];
-  bf16x8 qop[NT][4];
+  // This lane's column.
+  const int c_own = t.c0 + wave * COLS + col;
+  const bool active = t.c0 + wave * COLS < C, live = c_own < C;
+  const int i_own = live ? (int)a.by_g.quotient(c_own) : t.n - 1, h_own = live ? c_own - i_own * a.G : 0;
+  const int64_t row = (int64_t)(t.r0 + i_own) * a.Hq + t.g * a.G + h_own;
+  const Sight<MODE> sight = sight_of<MODE>(a, t, i_own);
+  bf16x8 qop[kQ];
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    const int c = cw + 16 * ct + col;
-    live[ct] = c < C;
-    const int i = live[ct] ? (int)a.by_g.quotient(c) : t.n - 1;
-    const int h = live[ct] ? c - i * a.G : 0;
-    row[ct] = (int64_t)(t.r0 + i) * a.Hq + t.g * a.G + h;
-    sight[ct] = sight_of<MODE>(a, t, i);
-    const uint16_t* src = a.q + row[ct] * kHeadDim + 8 * quad;
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      u32x4 x = *reinterpret_cast<const u32x4*>(src + 32 * kk);
-      if (!live[ct]) x = u32x4{0u, 0u, 0u, 0u};
-      qop[ct][kk] = __builtin_bit_cast(bf16x8, x);
-    }
+  for (int kk = 0; kk < kQ; ++kk) {
+    u32x4 x = *reinterpret_cast<const u32x4*>(a.q + row * kHeadDim + (kHeadDim / kQ) * kk + 8 * hi);
+    if (!live) x = u32x4{0u, 0u, 0u, 0u};
+    qop[kk] = __builtin_bit_cast(bf16x8, x);
   }
   int p0 = 0, p1 = 0;  // positions of the tile's first and last row
   if (MODE == RowsMode::kWindow) {
@@ -338,15 +346,11 @@ void rows_attn_kernel(RowsAttnArgs a) {
     p1 = max(base + (int)a.by_g.quotient(min(t.c0 + CT, C) - 1), 0);
   }
 
-  f32x4 acc[NT][kDimTiles];
-  float m[NT], l[NT];
+  f32x4 acc[kAcc];
 #pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    m[ct] = -INFINITY;
-    l[ct] = 0.f;
-#pragma unroll
-    for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
+  for (int j = 0; j < kAcc; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  float m = -INFINITY, l = 0.f;                // running maximum (in powers of two) and this lane's share of the sum
+  float minus_base = 0.f, limit = -INFINITY;   // -m (0 while nothing is seen); scores above this raise the maximum
 
   if (np > 0) {
     // Requests: wavefronts 0 and 1 bring the K tiles of a step's blocks, 2 and 3 the V tiles.
@@ -368,62 +372,93 @@ void rows_attn_kernel(RowsAttnArgs a) {
       }
       const uint64_t base = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(tile_hi, step & 63) << 32 |
                             (uint32_t)__builtin_amdgcn_readlane(tile_lo, step & 63);
-      fetch_4k<NT == 1>(base, lane_off, __builtin_amdgcn_readfirstlane(ring_at + at));
+      fetch_4k<!kWide>(base, lane_off, __builtin_amdgcn_readfirstlane(ring_at + at));
     };
 #pragma unroll
     for (int x = 0; x < kRing - 1; ++x) request(x, x * kStep);
-    f32x4 s[NT][2];
-    u32x4 pw[NT][kTerms];  // weights of the step as operands
-    int cur = 0;           // the step's place in the ring
+    float s[kTok];
+    u32x4 pw[kGroups][kTerms];  // weights of the step as operands
+    int cur = 0;                // the step's place in the ring
+    // Where this lane's fragments start: row `col` of a score product is block col / 16 [col / 8], slot
+    // 8 (col >> 2 & 1) + 4 (col >> 3 & 1) [+ 0, 4 for the second product] + (col & 3).
+    const char* k_frag = ring + (kWide ? col >> 4 : col >> 3) * (kTileBytes + 64) + hi * 256 +
+                         (8 * ((col >> 2) & 1) + (kWide ? 4 * ((col >> 3) & 1) : 0) + (col & 3)) * 16;
+    const char* v_frag = ring + kKStep + (col & 15) * 16 +
+                         (kWide ? (col >> 4) * 512 + hi * 256 : (hi >> 1) * kTileBytes + (hi & 1) * 256);
 
     auto scores = [&]() __attribute__((always_inline)) {
-      const char* kt = ring + cur + (col >> 3) * (kTileBytes + 64) + quad * 256 +
-                       (8 * ((col >> 2) & 1) + (col & 3)) * 16;
+      const char* kt = k_frag + cur;
+      if constexpr (kWide) {
+        f32x16 x = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) s[ct][0] = s[ct][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int kk = 0; kk < 8; ++kk)
+          x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const bf16x8*>(kt + 512 * kk), qop[kk], x,
+                                                      0, 0, 0);
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int e = 0; e < 16; ++e) s[e] = x[e];
+      } else {
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + 64 * x + 1024 * kk);
+        for (int y = 0; y < 2; ++y) {
+          f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int ct = 0; ct < NT; ++ct)
-            s[ct][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qop[ct][kk], s[ct][x], 0, 0, 0);
+          for (int kk = 0; kk < 4; ++kk)
+            x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<const bf16x8*>(kt + 64 * y + 1024 * kk),
+                                                        qop[kk], x, 0, 0, 0);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[4 * y + e] = x[e];
         }
-    };
-    auto weights = [&]() __attribute__((always_inline)) {
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        const float base = m[ct] == -INFINITY ? 0.f : m[ct];  // nothing seen yet
-        float sum[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          float x = exp2_of(fmaf(s[ct][e >> 1][2 * (e & 1)], a.scale, -base));
-          float y = exp2_of(fmaf(s[ct][e >> 1][2 * (e & 1) + 1], a.scale, -base));
-          sum[e] = x + y;
-          pw[ct][0][e] = bf16_pair(x, y);
-          if constexpr (kTerms == 3) {
-            x -= low_value(pw[ct][0][e]), y -= high_value(pw[ct][0][e]);
-            pw[ct][1][e] = bf16_pair(x, y);
-            x -= low_value(pw[ct][1][e]), y -= high_value(pw[ct][1][e]);
-            pw[ct][2][e] = bf16_pair(x, y);
-          }
-        }
-        l[ct] += (sum[0] + sum[1]) + (sum[2] + sum[3]);
       }
     };
+    // The step's weights as operands; this lane's sum of them.
+    auto weights = [&]() __attribute__((always_inline)) -> float {
+      float sum[kTok / 2];
+#pragma unroll
+      for (int e = 0; e < kTok / 2; ++e) {
+        const int g = e >> 2, at = e & 3;
+        float x = exp2_of(fmaf(s[2 * e], a.scale, minus_base));
+        float y = exp2_of(fmaf(s[2 * e + 1], a.scale, minus_base));
+        sum[e] = x + y;
+        pw[g][0][at] = bf16_pair(x, y);
+        if constexpr (kTerms == 3) {
+          x -= low_value(pw[g][0][at]), y -= high_value(pw[g][0][at]);
+          pw[g][1][at] = bf16_pair(x, y);
+          x -= low_value(pw[g][1][at]), y -= high_value(pw[g][1][at]);
+          pw[g][2][at] = bf16_pair(x, y);
+        }
+      }
+#pragma unroll
+      for (int n = kTok / 4; n >= 1; n /= 2)
+#pragma unroll
+        for (int e = 0; e < n; ++e) sum[e] += sum[e + n];
+      return sum[0];
+    };
     auto values = [&]() __attribute__((always_inline)) {
-      const char* vt = ring + cur + kKStep + (quad >> 1) * kTileBytes + (quad & 1) * 256 +
-                       col * 16;
+      const char* vt = v_frag + cur;
+      if constexpr (kWide) {
 #pragma unroll
-      for (int dt = 0; dt < kDimTiles; ++dt) {
-        const bf16x8 vf = *reinterpret_cast<const bf16x8*>(vt + 512 * dt);
+        for (int dt = 0; dt < 4; ++dt) {
+          f32x16 x;
 #pragma unroll
-        for (int ct = 0; ct < NT; ++ct)
+          for (int r = 0; r < 16; ++r) x[r] = acc[4 * dt + (r >> 2)][r & 3];
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            const bf16x8 vf = *reinterpret_cast<const bf16x8*>(vt + g * kTileBytes + 1024 * dt);
+#pragma unroll
+            for (int term = 0; term < kTerms; ++term)
+              x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, __builtin_bit_cast(bf16x8, pw[g][term]), x, 0, 0, 0);
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[4 * dt + (r >> 2)][r & 3] = x[r];
+        }
+      } else {
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+          const bf16x8 vf = *reinterpret_cast<const bf16x8*>(vt + 512 * dt);
 #pragma unroll
           for (int term = 0; term < kTerms; ++term)
-            acc[ct][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[ct][term]),
-                                                                  acc[ct][dt], 0, 0, 0);
+            acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, pw[0][term]), acc[dt],
+                                                              0, 0, 0);
+        }
       }
     };
     // A V tile that not every row sees whole, before the products read it: tokens outside the range are cleared
@@ -454,58 +489,51 @@ void rows_attn_kernel(RowsAttnArgs a) {
       const uint16_t* vt = a.v + kv_tile(blk_of, t.g, a.s.Hkv) * kTileElems;
 #pragma unroll 1
       for (int slot = 0; slot < kBlockSize; ++slot) {
-        const int tok = c.first + slot, from = (2 * x + (slot >> 3)) * 16 + col;
+        const int tok = c.first + slot;
         if (tok < c.t0 || tok >= c.t1) continue;
-        float w[NT];
+        const int from = ((kWide ? 0 : 2 * x) + (slot >> 3)) * COLS + col;  // the lane with this token's weight
+        float w = 0.f;
 #pragma unroll
-        for (int ct = 0; ct < NT; ++ct) {
-          w[ct] = 0.f;
-#pragma unroll
-          for (int term = 0; term < kTerms; ++term) {
-            const uint32_t w0 = pw[ct][term][0], w1 = pw[ct][term][1], w2 = pw[ct][term][2], w3 = pw[ct][term][3];
-            const uint32_t lo = slot & 4 ? w2 : w0, hi = slot & 4 ? w3 : w1;
-            const uint32_t pair = (uint32_t)__shfl((int)(slot & 2 ? hi : lo), from);
-            w[ct] += slot & 1 ? high_value(pair) : low_value(pair);
-          }
-          if (!seen<MODE>(a, rg, c, sight[ct], tok)) w[ct] = -1.f;
-        }
-#pragma unroll
-        for (int dt = 0; dt < kDimTiles; ++dt)
+        for (int term = 0; term < kTerms; ++term) {
+          uint32_t w4[4];
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            const uint32_t bits = vt[(16 * dt + 4 * quad + e) * kBlockSize + slot];
-            if ((bits & 0x7F80u) != 0x7F80u) continue;
+            const uint32_t lower = pw[0][term][e], upper = pw[kGroups - 1][term][e];
+            w4[e] = x ? upper : lower;
+          }
+          const uint32_t lo = slot & 4 ? w4[2] : w4[0], up = slot & 4 ? w4[3] : w4[1];
+          const uint32_t pair = (uint32_t)__shfl((int)(slot & 2 ? up : lo), from);
+          w += slot & 1 ? high_value(pair) : low_value(pair);
+        }
+        if (!seen<MODE>(a, rg, c, sight, tok)) w = -1.f;
 #pragma unroll
-            for (int ct = 0; ct < NT; ++ct)
-              if (!(w[ct] < 0.f)) acc[ct][dt][e] += w[ct] * low_value(bits);
+        for (int j = 0; j < kAcc; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const uint32_t bits = vt[(kStride * j + 4 * hi + e) * kBlockSize + slot];
+            const bool take = ((bits & 0x7F80u) == 0x7F80u) & !(w < 0.f);
+            acc[j][e] += take ? w * low_value(bits) : 0.f;
           }
       }
     };
 
     // The sums follow the maximum where a score exceeds it by more than the slack.
     auto raise_maximum = [&]() __attribute__((always_inline)) {
-      float top[NT];
-      bool raise = false;
+      float top = s[0];
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        top[ct] = s[ct][0][0];
+      for (int e = 1; e < kTok; ++e) top = fmaxf(top, s[e]);
+      if (__any(top > limit)) {
+        float x = top * a.scale;
+        if (!kWide) x = fmaxf(x, __shfl_xor(x, 16));
+        x = fmaxf(x, __shfl_xor(x, 32));
+        const float m_new = fmaxf(m, x);
+        minus_base = m_new == -INFINITY ? 0.f : -m_new;
+        const float alpha = exp2_of(m + minus_base);
+        m = m_new;
+        limit = (m + kSlack) / a.scale;
+        l *= alpha;
 #pragma unroll
-        for (int e = 1; e < 8; ++e) top[ct] = fmaxf(top[ct], s[ct][e >> 2][e & 3]);
-        raise |= fmaf(top[ct], a.scale, -kSlack) > m[ct];
-      }
-      if (__any(raise)) {
-#pragma unroll
-        for (int ct = 0; ct < NT; ++ct) {
-          float x = top[ct] * a.scale;
-          x = fmaxf(x, __shfl_xor(x, 16));
-          x = fmaxf(x, __shfl_xor(x, 32));
-          const float m_new = fmaxf(m[ct], x);
-          const float alpha = exp2_of(m[ct] - (m_new == -INFINITY ? 0.f : m_new));
-          m[ct] = m_new;
-          l[ct] *= alpha;
-#pragma unroll
-          for (int dt = 0; dt < kDimTiles; ++dt) acc[ct][dt] *= alpha;
-        }
+        for (int j = 0; j < kAcc; ++j) acc[j] *= alpha;
       }
     };
     auto next = [&](int i) __attribute__((always_inline)) {
@@ -538,19 +566,17 @@ void rows_attn_kernel(RowsAttnArgs a) {
         if constexpr (kComputes) {
           scores();
           if (part) {
-            const bool second = quad >= 2;  // this lane's block
-            const Block mine = {second ? now1.first : now0.first, second ? now1.t0 : now0.t0,
-                                second ? now1.t1 : now0.t1, second ? now1.tree : now0.tree};
 #pragma unroll
-            for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const bool ok = seen<MODE>(a, rg, mine, sight[ct], mine.first + 8 * (quad & 1) + e);
-                s[ct][e >> 2][e & 3] = ok ? s[ct][e >> 2][e & 3] : -INFINITY;
-              }
+            for (int e = 0; e < kTok; ++e) {
+              const bool second = kWide ? e >= 8 : hi >= 2;  // the token's block
+              const Block mine = {second ? now1.first : now0.first, second ? now1.t0 : now0.t0,
+                                  second ? now1.t1 : now0.t1, second ? now1.tree : now0.tree};
+              const bool ok = seen<MODE>(a, rg, mine, sight, mine.first + 8 * (hi & 1) + (e & 7));
+              s[e] = ok ? s[e] : -INFINITY;
+            }
           }
           raise_maximum();
-          weights();
+          l += weights();
           if (part) {
 #pragma unroll 1
             for (int x = odd_tile[0] ? 0 : 1; x < (odd_tile[1] ? 2 : 1); ++x) odd_values(x ? now1 : now0, x);
@@ -566,20 +592,16 @@ void rows_attn_kernel(RowsAttnArgs a) {
   }
 
   if (!active) return;
-#pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    float sum = l[ct];
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (!live[ct]) continue;
-    if (a.nc == 1) {
-      store_row<BF16>(a.out, a.lse, row[ct], acc[ct], sum, m[ct], quad);
-    } else if (np > 0) {  // a chunk's partial rows
-      const int64_t base = (int64_t)chunk * a.rows * a.Hq;
-      store_row<false>(a.part_out + base * kHeadDim, a.part_lse + base, row[ct], acc[ct], sum, m[ct], quad);
-    } else if (quad == 0) {
-      a.part_lse[(int64_t)chunk * a.rows * a.Hq + row[ct]] = -INFINITY;
-    }
+  if (!kWide) l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (!live) return;
+  if (a.nc == 1) {
+    store_row<BF16, kStride>(a.out, a.lse, row, acc, l, m, 4 * hi);
+  } else if (np > 0) {  // a chunk's partial row
+    const int64_t base = (int64_t)chunk * a.rows * a.Hq;
+    store_row<false, kStride>(a.part_out + base * kHeadDim, a.part_lse + base, row, acc, l, m, 4 * hi);
+  } else if (hi == 0) {
+    a.part_lse[(int64_t)chunk * a.rows * a.Hq + row] = -INFINITY;
   }
 }
 
@@ -654,8 +676,8 @@ __global__ __launch_bounds__(32 * (KP < 8 ? 8 : KP)) void rows_merge_kernel(Rows
 template <RowsMode MODE, bool BF16>
 void launch_tiles(const RowsAttnArgs& a, hipStream_t stream) {
   const dim3 grid(a.tiles * (unsigned)a.nc), block(64 * W);
-  if (a.tile == kRowsTile) hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 2>), grid, block, 0, stream, a);
-  else hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 1>), grid, block, 0, stream, a);
+  if (a.tile == kRowsTile) hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 32>), grid, block, 0, stream, a);
+  else hipLaunchKernelGGL((rows_attn_kernel<MODE, BF16, 16>), grid, block, 0, stream, a);
 }
 
 template <bool BF16>
@@ -673,8 +695,13 @@ hipError_t launch_rows_attn(const RowsAttnArgs& args, RowsMode mode, bool bf16, 
   RowsAttnArgs a = args;
   a.tiles = (unsigned)((int64_t)a.rows * a.G / a.tile + a.s.B) * (unsigned)a.s.Hkv;
   a.by_tiles.set(a.tiles);
-  if (mode == RowsMode::kTree) bf16 ? launch_tiles<RowsMode::kTree, true>(a, stream) : launch_tiles<RowsMode::kTree, false>(a, stream);
-  else bf16 ? launch_tiles<RowsMode::kWindow, true>(a, stream) : launch_tiles<RowsMode::kWindow, false>(a, stream);
+  if (mode == RowsMode::kTree) {
+    if (bf16) launch_tiles<RowsMode::kTree, true>(a, stream);
+    else launch_tiles<RowsMode::kTree, false>(a, stream);
+  } else {
+    if (bf16) launch_tiles<RowsMode::kWindow, true>(a, stream);
+    else launch_tiles<RowsMode::kWindow, false>(a, stream);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nc == 1) return e;
   if (bf16) launch_merge_rows<true>(a, stream);

@@ -38,8 +38,8 @@ __device__ __forceinline__ int block_of_flat(const int32_t* __restrict__ row, co
 // writes 8 tokens of one dim with one store.  Blocks that the new tokens cover in part are written element by
 // element.  The x-th block of sequence b is workgroup floor(row_begin[b] / 16) + 2 b + x of its head: n rows
 // touch at most floor(n / 16) + 2 blocks.
-// Measured on MI355X: 48 single tokens 4.4 us, prompts of 8,000 tokens together (8 kv heads, 88 MB) 25 us;
-// a workgroup per row, two bytes of V per store, took 88.
+// HBM-bound.  Measured on MI355X: 48 single tokens 4.4 us, prompts of 8,000 tokens together (8 kv heads, 88 MB)
+// 18 us, 4.9 TB/s (a copy reaches 4.75); V element by element 25, a workgroup per row, two bytes of V a store, 88.
 __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict__ k_rows,
                                                      const uint16_t* __restrict__ v_rows, int rows,
                                                      const int32_t* __restrict__ row_begin,
@@ -60,7 +60,8 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
   if (blk < 0) return;
   const int64_t tile = kv_tile(blk, g, s.Hkv) * kTileElems;
   // Slots [lo, hi) of the block are new; slot x is row r0 + j 16 + x - t0.
-  const int lo = (int)max(from - j * kBlockSize, (int64_t)0), hi = (int)min(t0 + n - j * kBlockSize, (int64_t)kBlockSize);
+  const int lo = (int)max(from - j * kBlockSize, (int64_t)0);
+  const int hi = (int)min(t0 + n - j * kBlockSize, (int64_t)kBlockSize);
   const int64_t row0 = r0 + j * kBlockSize - t0;
   {
     const int x = threadIdx.x >> 4, ch = threadIdx.x & 15;
@@ -100,6 +101,12 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 //  * V: kPlaces places for a wavefront, counted from a multiple of 8 tokens.  The blocks they come from (256 bytes
 //    each for 8 dims, each read once) pass through LDS, kParts at a time; a lane then gathers 8 places of one dim
 //    and writes them with one store.
+// HBM-bound where every place moves.  Measured on MI355X: 6 sequences of 9000 tokens, every second one kept, 8 kv
+// heads: 86 us for 331 MB (blocks are read whole; 221 MB are kept tokens read and written), 3.9 TB/s.  A workgroup
+// for each (sequence, kv head), as below, took 490.
+//
+// Few kept tokens leave most of these lanes idle: 48 sequences that keep up to 7 of 48 take 7.1 us here, 4.5 in the
+// kernel below, which reads V element by element but has all of a token's dims under way at once.
 constexpr int kFewKept = 64;  // up to here the kernel for few tokens
 constexpr int kCompactWaves = 4;
 constexpr int kKeyUnroll = 4;
@@ -340,9 +347,9 @@ hipError_t launch_append(const void* k_rows, const void* v_rows, int rows, const
   const unsigned places = (unsigned)(rows / kBlockSize) + 2 * (unsigned)s.B;
   FastDiv by_hkv;
   by_hkv.set((uint32_t)s.Hkv);
-  hipLaunchKernelGGL(append_kernel, dim3(places * (unsigned)s.Hkv), dim3(256), 0, stream, static_cast<const uint16_t*>(k_rows),
-                     static_cast<const uint16_t*>(v_rows), rows, row_begin, first, table, static_cast<uint16_t*>(k),
-                     static_cast<uint16_t*>(v), s, by_hkv);
+  hipLaunchKernelGGL(append_kernel, dim3(places * (unsigned)s.Hkv), dim3(256), 0, stream,
+                     static_cast<const uint16_t*>(k_rows), static_cast<const uint16_t*>(v_rows), rows, row_begin, first,
+                     table, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), s, by_hkv);
   return hipGetLastError();
 }
 
@@ -353,8 +360,8 @@ hipError_t launch_compact(void* k, void* v, const int32_t* table, const int32_t*
     hipLaunchKernelGGL(compact_few_kernel, dim3(pairs), dim3(256), 0, stream, static_cast<uint16_t*>(k),
                        static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
   else
-    hipLaunchKernelGGL(compact_kernel, dim3(pairs * 32u), dim3(64 * kCompactWaves), 0, stream, static_cast<uint16_t*>(k),
-                       static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
+    hipLaunchKernelGGL(compact_kernel, dim3(pairs * 32u), dim3(64 * kCompactWaves), 0, stream,
+                       static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
   return hipGetLastError();
 }
 

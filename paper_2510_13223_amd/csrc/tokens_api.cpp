@@ -90,14 +90,15 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
 // 13 nodes, groups of 4, fp32: 108 -> 80 us), and the loads go past the caches, as no other tile reads them.
 //
 // A tile's list of steps (32 tokens) is cut into chunks where that is estimated to be faster.  With n
-// workgroups at work, of at most `slots`, a step takes max(latency, n x kStepNs): alone it is bound by the chain of
+// workgroups at work, of at most `slots`, a step takes max(latency, n x step_us): alone it is bound by the chain of
 // its products, all together by HBM or the matrix and vector units.  Each workgroup's start costs it
-// kStartSteps more; the last chunks run on while the GPU empties, a quarter of a chunk's latency on the mean; each chunk's partial rows are written and read once more, after a
-// launch.  Times in us, measured on MI355X (kStepNs: the whole call's time per step, ns):
+// kStartSteps more; the last chunks run on while the GPU empties, a quarter of a chunk's latency on the mean; each
+// chunk's partial rows are written and read once more, after a launch.  Times in us, measured on MI355X (step_us is
+// the whole call's time per step, here in ns):
 //   64 columns, bf16 / fp32:  2.5 / 2.7     128 columns, bf16 / fp32:  2.2 / 4.4     latency of a step 0.7
-// Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.8; 64 rows, window 4096, 202
-// -> 173; 2048 rows x 64 heads, 3200 to 12800 tokens, 656 -> 629; prompts of 750 rows, window 512, stay whole (58,
-// in two chunks 89).
+// Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.9; 64 rows, window 4096, 199
+// -> 176; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750 rows, window 512, stay whole (55,
+// in two chunks 86).
 struct RowsPlan {
   int nc = 1;
   int least = 1;  // steps of a chunk at least
@@ -237,7 +238,8 @@ bana_status bana_window_attn(const bana_dims* d, int64_t rows, const int32_t* ro
   a.seq_lens = seq_lens;
   a.window = window;
   a.sinks = sinks;
-  set_plan(a, d, plan_rows(d, rows, window_tokens(d, window, sinks), out_type == BANA_OUT_BF16), workspace, workspace_bytes);
+  const RowsPlan p = plan_rows(d, rows, window_tokens(d, window, sinks), out_type == BANA_OUT_BF16);
+  set_plan(a, d, p, workspace, workspace_bytes);
   return device_status(bana::launch_rows_attn(a, bana::RowsMode::kWindow, out_type == BANA_OUT_BF16,
                                               static_cast<hipStream_t>(stream)));
 }
@@ -285,6 +287,7 @@ bana_status bana_reserve_kv_blocks(const bana_dims* d, int32_t* block_table, con
       !aligned16(block_refs) || workspace_bytes < bana_kv_blocks_workspace_bytes(d))
     return BANA_ERR_INVALID;
   if (d->num_blocks > INT32_MAX) return BANA_ERR_UNSUPPORTED;  // table entries are 32-bit
+  if ((int64_t)d->batch * d->max_blocks_per_seq > INT32_MAX) return BANA_ERR_UNSUPPORTED;  // 32-bit sums of entries
   return device_status(bana::launch_reserve(block_table, seq_lens, need_lens, block_refs, d->num_blocks, status,
                                             static_cast<int32_t*>(workspace), shape_of(d),
                                             static_cast<hipStream_t>(stream)));

@@ -107,6 +107,7 @@ void check_blocks(const int32_t* table, const int32_t* refs, int64_t num_blocks,
 hipError_t launch_reserve(int32_t* table, const int32_t* lens, const int32_t* need, int32_t* refs, int64_t num_blocks,
                           int32_t* status, int32_t* ws, CacheShape s, hipStream_t) {
   check_blocks(table, refs, num_blocks, status, ws, s);
+  REQUIRE((int64_t)s.B * s.max_blocks <= INT32_MAX);
   REQUIRE(ws && inside(lens, (unsigned __int128)s.B * 4) && inside(need, (unsigned __int128)s.B * 4));
   return hipSuccess;
 }

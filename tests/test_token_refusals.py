@@ -110,6 +110,7 @@ def test_bad_sizes_and_kinds(lib):
     assert call(lib, "fork_kv_seqs", {3: 0}) == 0
     for name in ("reserve_kv_blocks", "fork_kv_seqs", "release_kv_blocks"):
         assert call(lib, name, d=dims(num_blocks=1 << 31)) == -2
+    assert call(lib, "reserve_kv_blocks", d=dims(batch=1 << 10, max_blocks_per_seq=1 << 21)) == -2
     need = lib.bana_kv_blocks_workspace_bytes(ctypes.byref(dims()))
     assert need >= 4 * 100
     for name, at in (("reserve_kv_blocks", 7), ("fork_kv_seqs", 11)):
