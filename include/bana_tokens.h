@@ -102,7 +102,7 @@ bana_status bana_append_kv(const bana_dims* d, int64_t rows, const int32_t* row_
  * kept[b][0] >= 0 on (an accepted path among drafted tokens, or what an eviction leaves of a sequence).
  * The tokens behind the last one moved keep what they held.  The blocks written must belong to one
  * sequence only.  Tokens outside the table or in no block of the pool are skipped.  BANA_ERR_UNSUPPORTED:
- * batch * num_kv_heads above 2^18.
+ * batch * num_kv_heads above 2^18, max_kept of 2^30 or more.
  *   kept    int32 [batch][max_kept]
  *   n_kept  int32 [batch], clamped to [0, max_kept]
  */

@@ -539,6 +539,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
     auto next = [&](int i) __attribute__((always_inline)) {
       // Everybody's tiles of this step are there, and nobody reads those of the step before.
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((kRing - 2) * kLoads) : "memory");
+      race_check_delay(wave);
       request(i + kRing - 1, cur == 0 ? (kRing - 1) * kStep : cur - kStep);
     };
     auto walk = [&](auto computes) __attribute__((always_inline)) {
@@ -558,6 +559,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
           if (part) {
             now0 = block_at<MODE>(a, rg, c, v, p0, p1);
             now1 = block_at<MODE>(a, rg, c, v + 1, p0, p1);
+            race_check_delay(wave);
             if (is_v) clean(x_of ? now1.first : now0.first, x_of ? now1.t0 : now0.t0, x_of ? now1.t1 : now0.t1);
             asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
           }

@@ -142,6 +142,7 @@ __device__ __forceinline__ void compact_keys(uint16_t* __restrict__ k, const int
   for (int base = 0; base < n; base += kStep) {
     u32x4 key[kKeyUnroll];
     int64_t at[kKeyUnroll];
+    race_check_delay(wave);
 #pragma unroll
     for (int u = 0; u < kKeyUnroll; ++u) {
       at[u] = to[u];
@@ -224,6 +225,7 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
       last = __shfl(before, 63);
     }
     const bool any = __any(moves);
+    race_check_delay(wave);
     u16x8 val[U] = {}, from[U];
     int64_t to[U];
     wave_lds_fence();
@@ -319,6 +321,7 @@ __global__ __launch_bounds__(256) void compact_few_kernel(uint16_t* __restrict__
       }
     }
     const bool move = to >= 0 && of >= 0;
+    race_check_delay(threadIdx.x >> 6);
     u32x4 key;
     u16x8 val;
     if (move) {

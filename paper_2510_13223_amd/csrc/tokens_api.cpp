@@ -26,6 +26,7 @@ constexpr int64_t kMaxHeadRows = int64_t{1} << 26;       // rows x heads
 constexpr int64_t kMaxPairs = int64_t{1} << 23;          // batch x kv heads of an attention: its workgroups likewise
 constexpr int64_t kMaxTokenPairs = int64_t{1} << 18;     // of append and compact: 32 workgroups each in 32 bits
 constexpr int kMaxForks = 1 << 20;                       // 8 workgroups each in 32 bits
+constexpr int kMaxKept = 1 << 30;                        // places of a step past the list's end in 32 bits
 constexpr int kMaxTreeParts = 63;                        // ranges of a tree call: with the nodes, one per lane
 constexpr int64_t kMaxLaunchItems = UINT32_MAX;          // work-items of one launch
 constexpr int kMaxChunks = 128;
@@ -267,7 +268,7 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
   if (!k_cache || !v_cache || !block_table || !first_token || !kept || !n_kept || max_kept < 0)
     return BANA_ERR_INVALID;
   if (!aligned16(k_cache) || !aligned16(v_cache)) return BANA_ERR_INVALID;
-  if ((int64_t)d->batch * d->num_kv_heads > kMaxTokenPairs) return BANA_ERR_UNSUPPORTED;
+  if ((int64_t)d->batch * d->num_kv_heads > kMaxTokenPairs || max_kept >= kMaxKept) return BANA_ERR_UNSUPPORTED;
   if (max_kept == 0) return BANA_OK;
   return device_status(bana::launch_compact(k_cache, v_cache, block_table, first_token, kept, max_kept, n_kept,
                                             shape_of(d), static_cast<hipStream_t>(stream)));

@@ -208,11 +208,12 @@ def test_rows_before_the_first_position_see_nothing():
     assert bool((out[:5] == 0).all()) and bool((lse[:5] == -math.inf).all())
 
 
+@pytest.mark.parametrize("nodes", [24, 12])  # tiles of 128 columns and of 64
 @pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
-def test_values_that_a_row_does_not_see_never_reach_it(bad):
+def test_values_that_a_row_does_not_see_never_reach_it(bad, nodes):
     """A node and a token whose key and value are not finite: the rows that do not see them are as without them."""
-    cache, q, rb, begin, end, at, masks = tree_case((8, 2, [50], [24], 1), 19)
-    masks = masks[:1] + [1 << i | (1 if i % 2 else 0) for i in range(24)] + masks[25:]
+    cache, q, rb, begin, end, at, masks = tree_case((8, 2, [50], [nodes], 1), 19)
+    masks = masks[:1] + [1 << i | (1 if i % 2 else 0) for i in range(nodes)] + masks[nodes + 1:]
     clean = [run_tree(cache, q, rb, begin, end, at, masks, 0.1, bf16) for bf16 in (False, True)]
     cache.values[0][50 + 6] = bad
     cache.keys[0][50 + 7] = bad

@@ -106,6 +106,7 @@ def test_bad_sizes_and_kinds(lib):
     assert call(lib, "window_attn", {11: -1}) == -1
     assert call(lib, "window_attn", {8: FAKE}) == -1 and call(lib, "window_attn", {9: FAKE}) == -1
     assert call(lib, "compact_kv_tokens", {6: -1}) == -1 and call(lib, "compact_kv_tokens", {6: 0}) == 0
+    assert call(lib, "compact_kv_tokens", {6: 1 << 30}) == -2
     assert call(lib, "fork_kv_seqs", {3: -1}) == -1 and call(lib, "fork_kv_seqs", {3: 5}) == -1
     assert call(lib, "fork_kv_seqs", {3: 0}) == 0
     for name in ("reserve_kv_blocks", "fork_kv_seqs", "release_kv_blocks"):
