@@ -628,7 +628,13 @@ __global__ __launch_bounds__(32 * (KP < 8 ? 8 : KP)) void rows_merge_kernel(Rows
       for (int u = 0; u < 4; ++u) {
         const int c = min(c0 + u * KP, a.nc - 1);
         x[u] = a.part_lse[c * n + r];
-        v[u] = reinterpret_cast<const f32x4*>(a.part_out + (c * n + r) * kHeadDim)[lane];
+        if (KP > 1) v[u] = reinterpret_cast<const f32x4*>(a.part_out + (c * n + r) * kHeadDim)[lane];
+      }
+      if (KP == 1) {  // many rows: only the parts that are not empty (24 ragged drafts 78.6 -> 76.8 us)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          if (x[u] != -INFINITY)
+            v[u] = reinterpret_cast<const f32x4*>(a.part_out + (min(c0 + u, a.nc - 1) * n + r) * kHeadDim)[lane];
       }
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
