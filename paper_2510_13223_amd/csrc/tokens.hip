@@ -93,7 +93,7 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 }
 
 // Tokens move along their own axis only, so the 8 dims of a K chunk, and any 8 dims of V, of one sequence and kv
-// head are moved without regard to any other: 32 workgroups of four wavefronts for each (sequence, kv head).  In
+// head are moved without regard to any other: 32 workgroups of W wavefronts for each (sequence, kv head).  In
 // a step the wavefronts take consecutive places of the list, and all have read before any writes; as
 // kept[i] >= i, a later step reads nothing that this one writes.  The next step's kept tokens and their blocks
 // are looked up meanwhile, without branches, so that many lookups are under way at once.
@@ -108,15 +108,19 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 // Few kept tokens leave most of these lanes idle: 48 sequences that keep up to 7 of 48 take 7.1 us here, 4.5 in the
 // kernel below, which reads V element by element but has all of a token's dims under way at once.
 constexpr int kFewKept = 64;  // up to here the kernel for few tokens
-constexpr int kCompactWaves = 4;
+
+// Wavefronts of a workgroup: 8 where that leaves at most one workgroup to a CU (1 sequence of 30000 tokens, half
+// kept: 83 us, with 4 99), else 4, three of which fit on a CU (6 of 9000: 86, with 8 164).
+constexpr unsigned kFewGroups = 256;
 constexpr int kKeyUnroll = 4;
 constexpr int kPlaces = 128;  // of a wavefront's V step
 constexpr int kParts = 32;    // source blocks of a wavefront in LDS
 
+template <int W>
 __device__ __forceinline__ void compact_keys(uint16_t* __restrict__ k, const int32_t* __restrict__ table,
                                              const int32_t* __restrict__ kept, int n, int64_t t0, int b, int g, int ch,
                                              const CacheShape& s) {
-  constexpr int kOwn = 64 * kKeyUnroll, kStep = kOwn * kCompactWaves;
+  constexpr int kOwn = 64 * kKeyUnroll, kStep = kOwn * W;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int32_t* row = table + (int64_t)b * s.max_blocks;
   int64_t to[kKeyUnroll], of[kKeyUnroll];
@@ -162,14 +166,15 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_wave_barrier();
 }
 
+template <int W>
 __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const int32_t* __restrict__ table,
                                                const int32_t* __restrict__ kept, int n, int64_t t0, int b, int g,
                                                int dims, const CacheShape& s) {
   constexpr int U = kPlaces / 64;
-  constexpr int kStep = kPlaces * kCompactWaves;
-  __shared__ __attribute__((aligned(16))) uint16_t sm_parts[kCompactWaves][kParts * 128];  // [block][8 dims][16 tokens]
-  __shared__ __attribute__((aligned(16))) uint16_t sm_froms[kCompactWaves][kPlaces];  // 16 x block's number + slot
-  __shared__ int32_t sm_blocks[kCompactWaves][kPlaces];                               // pool block of each number
+  constexpr int kStep = kPlaces * W;
+  __shared__ __attribute__((aligned(16))) uint16_t sm_parts[W][kParts * 128];  // [block][8 dims][16 tokens]
+  __shared__ __attribute__((aligned(16))) uint16_t sm_froms[W][kPlaces];  // 16 x block's number + slot
+  __shared__ int32_t sm_blocks[W][kPlaces];                               // pool block of each number
   constexpr uint16_t kNone = 0xFFFF;                                                  // no source
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = lane >> 3, h = lane & 7;
   uint16_t* sm_part = sm_parts[wave];
@@ -286,17 +291,18 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
   }
 }
 
-__global__ __launch_bounds__(64 * kCompactWaves) void compact_kernel(uint16_t* __restrict__ k, uint16_t* __restrict__ v,
-                                                     const int32_t* __restrict__ table,
-                                                     const int32_t* __restrict__ first,
-                                                     const int32_t* __restrict__ kept, int max_kept,
-                                                     const int32_t* __restrict__ n_kept, CacheShape s) {
+template <int W>
+__global__ __launch_bounds__(64 * W) void compact_kernel(uint16_t* __restrict__ k, uint16_t* __restrict__ v,
+                                                         const int32_t* __restrict__ table,
+                                                         const int32_t* __restrict__ first,
+                                                         const int32_t* __restrict__ kept, int max_kept,
+                                                         const int32_t* __restrict__ n_kept, CacheShape s) {
   const int part = (int)(blockIdx.x & 31), pair = (int)(blockIdx.x >> 5);  // 16 K chunks, then 16 groups of V dims
   const int b = pair / s.Hkv, g = pair - b * s.Hkv;
   const int n = min(max(n_kept[b], 0), max_kept);
   const int32_t* list = kept + (int64_t)b * max_kept;
-  if (part < 16) compact_keys(k, table, list, n, first[b], b, g, part, s);
-  else compact_values(v, table, list, n, first[b], b, g, part - 16, s);
+  if (part < 16) compact_keys<W>(k, table, list, n, first[b], b, g, part, s);
+  else compact_values<W>(v, table, list, n, first[b], b, g, part - 16, s);
 }
 
 // Few tokens: one workgroup per (sequence, kv head), 16 kept tokens at a time, a thread for each token and 8 dims.
@@ -362,9 +368,12 @@ hipError_t launch_compact(void* k, void* v, const int32_t* table, const int32_t*
   if (max_kept <= kFewKept)
     hipLaunchKernelGGL(compact_few_kernel, dim3(pairs), dim3(256), 0, stream, static_cast<uint16_t*>(k),
                        static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
+  else if (pairs * 32u <= kFewGroups)
+    hipLaunchKernelGGL((compact_kernel<8>), dim3(pairs * 32u), dim3(64 * 8), 0, stream, static_cast<uint16_t*>(k),
+                       static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
   else
-    hipLaunchKernelGGL(compact_kernel, dim3(pairs * 32u), dim3(64 * kCompactWaves), 0, stream,
-                       static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
+    hipLaunchKernelGGL((compact_kernel<4>), dim3(pairs * 32u), dim3(64 * 4), 0, stream, static_cast<uint16_t*>(k),
+                       static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
   return hipGetLastError();
 }
 
