@@ -258,7 +258,7 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // instructions and 16 exponentials, 16 KiB of LDS reads; three workgroups on a CU overlap them, in part.  2 x 4096 new
 // tokens, 32 heads, window 4096, bf16: 545 us, 1.03 PFLOP/s, where a library product of 8192^3 reaches 1.47; without
 // the weights' computation 444, without the LDS reads 498, without both 401.  32 trees of 64 nodes over 8000 tokens,
-// 64 heads: 625 us.  Instructions of 16 x 16 x 32 for 32 columns: 543, 640; 64 columns a wavefront, one per
+// 64 heads: 620 us.  Instructions of 16 x 16 x 32 for 32 columns: 543, 635; 64 columns a wavefront, one per
 // SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
 // 16 columns: HBM.  64 single tokens, window 4096: 176 us, 6.1 TB/s.
 constexpr int kTileBytes = kTileElems * 2;
@@ -317,7 +317,9 @@ void rows_attn_kernel(RowsAttnArgs a) {
   const int lane = threadIdx.x & 63, col = lane & (COLS - 1), hi = lane / COLS;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const unsigned chunk = a.by_tiles.quotient(blockIdx.x);
-  const Tile t = find_tile<CT>(a, blockIdx.x - chunk * a.tiles, lane);
+  // The last tiles of a prompt see the most tokens: they start first, so that short ones fill the end (a prompt of
+  // 8000 tokens 568 -> 516 us, six of 750, window 512, 55 -> 46).
+  const Tile t = find_tile<CT>(a, a.tiles - 1 - (blockIdx.x - chunk * a.tiles), lane);
   if (!t.any) return;
   const int C = t.n * a.G;
   const Ranges rg = find_ranges<MODE>(a, t, t.c0, min(t.c0 + CT, C), lane);
