@@ -245,21 +245,22 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 //           [8 tiles of 16 dims, one product of the 32 tokens]
 // A value product takes 8 consecutive tokens from each lane: slots 8 (hi & 1) + [0, 8) of a block, hi = lane / COLS.
 // The rows of the score products are assigned to tokens so that they leave exactly these in that lane, and P
-// never leaves it.  Every fragment is one 16-byte LDS read per lane, no two lanes of a phase on the same bank:
-// the second block's K tile lies 64 bytes off (16 columns read both blocks at once); of V, each 16 dims hold the
-// first 8 tokens of all dims, then the last 8.
+// never leaves it.  Every fragment is one 16-byte LDS read per lane, no two lanes of a phase (0-3, 12-15, 20-23, 24-27
+// and so on) on the same bank: with 16 columns the second block's K tile lies 64 bytes off, with 32 it must not (it cost
+// a third of the LDS cycles); of V, each 16 dims hold the first 8 tokens of all dims, then the last 8.
 //
 // The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
 // changes no relative rounding), which spares most steps the rescaling of the sums.  A bf16 result takes its weights
 // rounded to bf16, half a step of the result's own type; an fp32 result takes them as three bf16 terms, 24 bits.
 // Their sum is of the unrounded ones in both.
 //
-// What bounds it, 32 columns: 16 matrix instructions of 32 cycles a step and wavefront, some 80 vector
-// instructions and 16 exponentials, 16 KiB of LDS reads; three workgroups on a CU overlap them, in part.  2 x 4096 new
-// tokens, 32 heads, window 4096, bf16: 545 us, 1.03 PFLOP/s, where a library product of 8192^3 reaches 1.47; without
-// the weights' computation 444, without the LDS reads 498, without both 401.  32 trees of 64 nodes over 8000 tokens,
-// 64 heads: 620 us.  Instructions of 16 x 16 x 32 for 32 columns: 543, 635; 64 columns a wavefront, one per
-// SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
+// What bounds it, 32 columns: the matrix and vector units, at the clock that the card's power leaves them.  A step of
+// a wavefront is 16 matrix instructions of 32 cycles, some 80 vector instructions and 16 exponentials, and 16 KiB of
+// LDS reads; three workgroups on a CU overlap them in part.  2 x 4096 new tokens, 32 heads, window 4096, bf16: 537 to
+// 560 us, 1.0 PFLOP/s, where a library product of 8192^3 reaches 1.47; the same call on zeros takes 425.  Without the
+// weights' computation 444, with one LDS fragment for all 498, without both 401.  32 trees of 64 nodes over 8000
+// tokens, 64 heads: 597 to 620 us.  Instructions of 16 x 16 x 32 for 32 columns: 2 % more; 64 columns a wavefront, one
+// per SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
 // 16 columns: HBM.  64 single tokens, window 4096: 176 us, 6.1 TB/s.
 constexpr int kTileBytes = kTileElems * 2;
 constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
@@ -312,6 +313,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
   constexpr int kStride = kWide ? 8 : 16;  // this lane's sums: dims kStride j + 4 hi + [0, 4)
   constexpr int kAcc = kHeadDim / kStride;
   constexpr int kQ = kWide ? 8 : 4;
+  constexpr int kApart = kWide ? 0 : 64;  // bytes between a step's K tiles
   __shared__ __attribute__((aligned(16))) char ring[kRing * kStep];
   __shared__ int odd_tile[2];  // a V tile had values that are not finite
   const int lane = threadIdx.x & 63, col = lane & (COLS - 1), hi = lane / COLS;
@@ -363,7 +365,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
     for (int x = 0; x < 4; ++x)
       lane_off[x] = 1024 * x + (is_v ? (lane >> 5) * 512 + (lane & 15) * 32 + ((lane >> 4) & 1) * 16 : lane * 16);
     const uint32_t ring_at = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring +
-                             (is_v ? kKStep : 64 * x_of) + x_of * kTileBytes;
+                             (is_v ? kKStep : kApart * x_of) + x_of * kTileBytes;
     const uint64_t pool = reinterpret_cast<uint64_t>(is_v ? a.v : a.k);
     uint32_t tile_lo = 0, tile_hi = 0;  // addresses of the wavefront's tiles, 64 steps at a time, one per lane
     auto request = [&](int step, int at) __attribute__((always_inline)) {  // into the ring at byte `at`
@@ -383,7 +385,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
     int cur = 0;                // the step's place in the ring
     // Where this lane's fragments start: row `col` of a score product is block col / 16 [col / 8], slot
     // 8 (col >> 2 & 1) + 4 (col >> 3 & 1) [+ 0, 4 for the second product] + (col & 3).
-    const char* k_frag = ring + (kWide ? col >> 4 : col >> 3) * (kTileBytes + 64) + hi * 256 +
+    const char* k_frag = ring + (kWide ? col >> 4 : col >> 3) * (kTileBytes + kApart) + hi * 256 +
                          (8 * ((col >> 2) & 1) + (kWide ? 4 * ((col >> 3) & 1) : 0) + (col & 3)) * 16;
     const char* v_frag = ring + kKStep + (col & 15) * 16 +
                          (kWide ? (col >> 4) * 512 + hi * 256 : (hi >> 1) * kTileBytes + (hi & 1) * 256);

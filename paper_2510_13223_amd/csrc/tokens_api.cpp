@@ -98,8 +98,8 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
 // the whole call's time per step, here in ns):
 //   64 columns, bf16 / fp32:  2.5 / 2.7     128 columns, bf16 / fp32:  2.2 / 4.4     latency of a step 0.7
 // Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.9; 64 rows, window 4096, 199
-// -> 176; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750 rows, window 512, stay whole (55,
-// in two chunks 86).
+// -> 176; 1 row over 16000 tokens 211 -> 19; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750
+// rows, window 512, stay whole (46, in two chunks 83).
 struct RowsPlan {
   int nc = 1;
   int least = 1;  // steps of a chunk at least
