@@ -246,8 +246,8 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // A value product takes 8 consecutive tokens from each lane: slots 8 (hi & 1) + [0, 8) of a block, hi = lane / COLS.
 // The rows of the score products are assigned to tokens so that they leave exactly these in that lane, and P
 // never leaves it.  Every fragment is one 16-byte LDS read per lane, no two lanes of a phase (0-3, 12-15, 20-23, 24-27
-// and so on) on the same bank: with 16 columns the second block's K tile lies 64 bytes off, with 32 it must not (it cost
-// a third of the LDS cycles); of V, each 16 dims hold the first 8 tokens of all dims, then the last 8.
+// and so on) on the same bank: with 16 columns the second block's K tile lies 64 bytes off, with 32 it must not (it
+// cost a third of the LDS cycles); of V, each 16 dims hold the first 8 tokens of all dims, then the last 8.
 //
 // The running maximum is raised only where a score exceeds it by 2^8 (the weights are then at most 2^8, which
 // changes no relative rounding), which spares most steps the rescaling of the sums.  A bf16 result takes its weights
