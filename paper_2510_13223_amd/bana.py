@@ -760,8 +760,8 @@ def bana_compact_kv_tokens(k_cache, v_cache, block_table, first_token, kept, n_k
         B, mb, nb, Hkv = _check_pools(k_cache, v_cache, block_table)
         _need(first_token, "first_token", torch.int32, (B,))
         _need(kept, "kept", torch.int32)
-        if kept.dim() != 2 or kept.shape[0] != B:
-            raise ValueError("kept must be [B, max_kept]")
+        if kept.dim() != 2 or kept.shape[0] != B or kept.shape[1] >= 1 << 31:
+            raise ValueError("kept must be [B, max_kept], max_kept a 32-bit number")
         _need(n_kept, "n_kept", torch.int32, (B,))
         _same_device(k_cache, v_cache, block_table, first_token, kept, n_kept)
         dims = bana_dims(B, Hkv, Hkv, HEAD_DIM, BLOCK_SIZE, mb, nb)

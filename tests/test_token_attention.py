@@ -332,6 +332,81 @@ def test_streams_and_graphs():
         torch.cuda.synchronize()
 
 
+def test_sixty_three_ranges():
+    """The most ranges a call may have, one per lane with the nodes: empty ones, single tokens, neighbours."""
+    rng = random.Random(53)
+    lens, news = [400, 70], [9, 30]
+    rb, rows = tc.rows_of(news)
+    cache, q = inputs([n + m for n, m in zip(lens, news)], 8, 2, rows, 59)
+    begin, end = [[0, 0] for _ in range(63)], [[0, 0] for _ in range(63)]
+    for b, n in enumerate(lens):
+        cuts = sorted(rng.sample(range(n), 63)) + [n]
+        for p in range(63):
+            begin[p][b], end[p][b] = cuts[p], rng.choice([cuts[p], cuts[p] + 1, cuts[p + 1], cuts[p + 1]])
+    masks = [m for n in news for m in tc.random_tree(n, rng)]
+    want = tc.attention(q, rb, cache, tc.tree_sees(begin, end, lens, masks, rb), 0.1)
+    for bf16 in (False, True):
+        tc.check_attention(*run_tree(cache, q, rb, begin, end, lens, masks, 0.1, bf16), want, bf16)
+
+
+def test_thousands_of_sequences():
+    """More than 64^2 sequences, most of them without a row: the search takes three rounds."""
+    rng = random.Random(61)
+    news = [rng.choice([0, 0, 0, 1]) for _ in range(4500)]
+    news[0], news[-1] = 2, 3
+    lens = [n + rng.randint(0, 3) for n in news]
+    rb, rows = tc.rows_of(news, pad=2, first=1)
+    cache, q = inputs(lens, 2, 1, rows, 67)
+    want = tc.attention(q, rb, cache, tc.window_sees(lens, news, 2, 1), 0.1)
+    out, lse = run_window(cache, q, rb, lens, 2, 1, 0.1, False)
+    same_outside(out, lse, rb)
+    tc.check_attention(*live_rows(out, lse, want, rb), False)
+
+
+def test_calls_at_once_with_workspaces_of_their_own():
+    """Two streams, then two graphs, each with its own workspace, under way together: the eager results each time."""
+    calls = []
+    for new, bf16, seed in ((3, True, 71), (50, False, 73)):
+        cache, q = inputs([3000, 900], 8, 2, 2 * new, seed)
+        dims = bana.make_dims(2, 8, 2, cache.table.shape[1], cache.num_blocks, max_range_tokens=3000,
+                              total_range_tokens=3900)
+        ws = workspace(bana.bana_window_attn_workspace_bytes(dims, 2 * new, 2500, 4))
+        assert ws is not None
+        args = (q.to(DEV), ints([0, new, 2 * new]), cache.k.to(DEV), cache.v.to(DEV), cache.table.to(DEV),
+                ints([3000, 900]), 2500, 4)
+        calls.append((args, results(2 * new, 8, bf16), dict(workspace=ws, dims=dims)))
+    eager = []
+    for args, outs, more in calls:
+        bana.bana_window_attn(*args, *outs, **more)
+        eager.append([x.clone() for x in outs])
+    torch.cuda.synchronize()
+
+    def both_as_eager():
+        torch.cuda.synchronize()
+        for (_, outs, _), want in zip(calls, eager):
+            for x, y in zip(outs, want):
+                assert torch.equal(x, y)
+                x.fill_(5.0)
+        torch.cuda.synchronize()
+
+    streams = [torch.cuda.Stream() for _ in calls]
+    both_as_eager()
+    for _ in range(10):
+        for s, (args, outs, more) in zip(streams, calls):
+            bana.bana_window_attn(*args, *outs, stream=s, **more)
+    both_as_eager()
+    graphs = []
+    for args, outs, more in calls:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            bana.bana_window_attn(*args, *outs, **more)
+    for _ in range(4):
+        for s, g in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                g.replay()
+        both_as_eager()
+
+
 def test_offsets_past_four_gigabytes():
     """A pool whose tiles lie past 2^32 bytes: the sequence's blocks at its far end."""
     hkv, n = 8, 150000  # 4.9 GB each of keys and values
