@@ -44,19 +44,24 @@ __device__ __forceinline__ float high_value(uint32_t pair) { return __builtin_bi
 // The columns [c0, c0 + CT) of sequence b and kv head g that a workgroup computes.
 struct Tile {
   int b, g, r0, n, c0;  // first row and number of rows of the sequence
+  int tokens;           // window: its tokens, in the table; tree: where its nodes begin
   bool any;             // some column exists
 };
 
-template <int CT>
+template <RowsMode MODE, int CT>
 __device__ __forceinline__ Tile find_tile(const RowsAttnArgs& a, unsigned wg, int lane) {
   const unsigned slot = a.by_hkv.quotient(wg);
-  auto first_slot = [&](int b) { return row_start(a.row_begin, b, a.rows) * a.G / CT + b; };
+  auto first_slot = [&](int b, int row) { return row * a.G / CT + b; };
   Tile t;
   t.g = (int)(wg - slot * a.s.Hkv);
-  t.b = last_at_most(a.s.B, (int)slot, lane, first_slot);
-  t.r0 = row_start(a.row_begin, t.b, a.rows);
-  t.n = row_start(a.row_begin, t.b + 1, a.rows) - t.r0;
-  t.c0 = ((int)slot - (t.r0 * a.G / CT + t.b)) * CT;
+  const SeqRows x = find_rows(a.row_begin, MODE == RowsMode::kTree ? a.tree_begin : a.seq_lens, a.rows, a.s.B, (int)slot,
+                              a.seqs_per_slot, lane, first_slot);
+  t.b = x.b;
+  t.r0 = x.begin;
+  t.n = x.end - x.begin;
+  const int span = a.s.max_blocks * kBlockSize;
+  t.tokens = MODE == RowsMode::kTree ? min(x.value, span) : min(max(x.value, 0), span);
+  t.c0 = ((int)slot - first_slot(x.b, x.begin)) * CT;
   t.any = t.c0 >= 0 && t.c0 < t.n * a.G;
   return t;
 }
@@ -107,7 +112,7 @@ __device__ __forceinline__ Ranges find_ranges(const RowsAttnArgs& a, const Tile&
   if (MODE == RowsMode::kTree) {
     r.count = a.n_parts + 1;
     r.tree = a.n_parts;
-    r.tree0 = min(a.tree_begin[t.b], span);
+    r.tree0 = t.tokens;
     if (lane < a.n_parts) {
       r.t0 = max(a.begin[(int64_t)lane * B + t.b], 0);
       r.t1 = min(a.end[(int64_t)lane * B + t.b], span);
@@ -118,7 +123,7 @@ __device__ __forceinline__ Ranges find_ranges(const RowsAttnArgs& a, const Tile&
   } else {
     r.count = 2;
     r.tree = r.tree0 = -1;
-    const int len = min(max(a.seq_lens[t.b], 0), span);
+    const int len = t.tokens;
     const int p0 = max(len - t.n + (int)a.by_g.quotient(ca), 0), p1 = max(len - t.n + (int)a.by_g.quotient(cb - 1), -1);
     const int lo = a.begin != nullptr ? max(a.begin[t.b], 0) : 0;
     const int hi = min(a.end != nullptr ? min(a.end[t.b], span) : span, p1 + 1);
@@ -211,7 +216,7 @@ __device__ __forceinline__ Sight<MODE> sight_of(const RowsAttnArgs& a, const Til
     s.nodes = a.mask[t.r0 + i];
     if (t.n < 64) s.nodes &= (uint64_t{1} << t.n) - 1;
   } else {
-    s.pos = max(min(max(a.seq_lens[t.b], 0), a.s.max_blocks * kBlockSize) - t.n + i, -1);
+    s.pos = max(t.tokens - t.n + i, -1);
   }
   return s;
 }
@@ -321,7 +326,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
   const unsigned chunk = a.by_tiles.quotient(blockIdx.x);
   // The last tiles of a prompt see the most tokens: they start first, so that short ones fill the end (a prompt of
   // 8000 tokens 568 -> 516 us, six of 750, window 512, 55 -> 46).
-  const Tile t = find_tile<CT>(a, a.tiles - 1 - (blockIdx.x - chunk * a.tiles), lane);
+  const Tile t = find_tile<MODE, CT>(a, a.tiles - 1 - (blockIdx.x - chunk * a.tiles), lane);
   if (!t.any) return;
   const int C = t.n * a.G;
   const Ranges rg = find_ranges<MODE>(a, t, t.c0, min(t.c0 + CT, C), lane);
@@ -345,7 +350,7 @@ void rows_attn_kernel(RowsAttnArgs a) {
   }
   int p0 = 0, p1 = 0;  // positions of the tile's first and last row
   if (MODE == RowsMode::kWindow) {
-    const int base = min(max(a.seq_lens[t.b], 0), a.s.max_blocks * kBlockSize) - t.n;
+    const int base = t.tokens - t.n;
     p0 = max(base + (int)a.by_g.quotient(t.c0), -1);
     p1 = max(base + (int)a.by_g.quotient(min(t.c0 + CT, C) - 1), 0);
   }
@@ -705,7 +710,9 @@ void launch_merge_rows(const RowsAttnArgs& a, hipStream_t stream) {
 
 hipError_t launch_rows_attn(const RowsAttnArgs& args, RowsMode mode, bool bf16, hipStream_t stream) {
   RowsAttnArgs a = args;
-  a.tiles = (unsigned)((int64_t)a.rows * a.G / a.tile + a.s.B) * (unsigned)a.s.Hkv;
+  const int64_t slots = (int64_t)a.rows * a.G / a.tile + a.s.B;
+  a.tiles = (unsigned)slots * (unsigned)a.s.Hkv;
+  a.seqs_per_slot = (float)a.s.B / (float)slots;
   a.by_tiles.set(a.tiles);
   if (mode == RowsMode::kTree) {
     if (bf16) launch_tiles<RowsMode::kTree, true>(a, stream);

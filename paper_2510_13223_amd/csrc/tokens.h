@@ -41,7 +41,9 @@ struct RowsAttnArgs {
   int nc, least, merge_groups;
   float* part_out;
   float* part_lse;
-  unsigned tiles;    // workgroups of a chunk (set by the launcher)
+  // Set by the launcher:
+  unsigned tiles;       // workgroups of a chunk
+  float seqs_per_slot;  // sequences per tile of a kv head
   FastDiv by_tiles;
 };
 

@@ -45,16 +45,18 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
                                                      const int32_t* __restrict__ row_begin,
                                                      const int32_t* __restrict__ first,
                                                      const int32_t* __restrict__ table, uint16_t* __restrict__ k,
-                                                     uint16_t* __restrict__ v, CacheShape s, FastDiv by_hkv) {
+                                                     uint16_t* __restrict__ v, CacheShape s, FastDiv by_hkv,
+                                                     float seqs_per_place) {
   constexpr int kPad = kHeadDim + 8;  // LDS row of a token: 16-byte pieces, rows 4 banks apart
   __shared__ __attribute__((aligned(16))) uint16_t sm_v[kBlockSize * kPad];
   const unsigned place = by_hkv.quotient(blockIdx.x);
   const int g = (int)(blockIdx.x - place * s.Hkv);
-  auto first_place = [&](int i) { return row_start(row_begin, i, rows) / kBlockSize + 2 * i; };
-  const int b = last_at_most(s.B, (int)place, threadIdx.x & 63, first_place);
-  const int r0 = row_start(row_begin, b, rows), n = row_start(row_begin, b + 1, rows) - r0;
-  const int64_t t0 = first[b];  // may be negative: those rows are skipped
-  const int64_t from = max(t0, (int64_t)0), j = (from >> 4) + ((int)place - first_place(b));
+  auto first_place = [](int i, int row) { return row / kBlockSize + 2 * i; };
+  const SeqRows x = find_rows(row_begin, first, rows, s.B, (int)place, seqs_per_place, threadIdx.x & 63,
+                              first_place);
+  const int b = x.b, r0 = x.begin, n = x.end - x.begin;
+  const int64_t t0 = x.value;  // may be negative: those rows are skipped
+  const int64_t from = max(t0, (int64_t)0), j = (from >> 4) + ((int)place - first_place(b, r0));
   if (j < (from >> 4) || j * kBlockSize >= t0 + n) return;
   const int blk = block_of(table, s, b, j * kBlockSize);
   if (blk < 0) return;
@@ -358,7 +360,8 @@ hipError_t launch_append(const void* k_rows, const void* v_rows, int rows, const
   by_hkv.set((uint32_t)s.Hkv);
   hipLaunchKernelGGL(append_kernel, dim3(places * (unsigned)s.Hkv), dim3(256), 0, stream,
                      static_cast<const uint16_t*>(k_rows), static_cast<const uint16_t*>(v_rows), rows, row_begin, first,
-                     table, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), s, by_hkv);
+                     table, static_cast<uint16_t*>(k), static_cast<uint16_t*>(v), s, by_hkv,
+                     (float)s.B / (float)places);
   return hipGetLastError();
 }
 
