@@ -16,8 +16,8 @@ struct SeqRows {
 };
 
 // The last b in [0, B) with first(b, row_begin[b]) <= x, first increasing (0 if there is none), for every lane of the
-// wavefront.  One load looks at 64 neighbours of where it would be if all sequences had as many rows (x * per_x), and at
-// their values, and mostly settles it; otherwise each round looks at 64 places of the remaining range, so 4096
+// wavefront.  One load looks at 64 neighbours of where it would be if all sequences had as many rows (x * per_x), and
+// at their values, and mostly settles it; otherwise each round looks at 64 places of the remaining range, so 4096
 // sequences take two more.  (2048 single tokens, window 64: 203 us, by rounds alone 217.)
 template <typename F>
 __device__ __forceinline__ SeqRows find_rows(const int32_t* __restrict__ row_begin, const int32_t* __restrict__ values,

@@ -54,8 +54,8 @@ __device__ __forceinline__ Tile find_tile(const RowsAttnArgs& a, unsigned wg, in
   auto first_slot = [&](int b, int row) { return row * a.G / CT + b; };
   Tile t;
   t.g = (int)(wg - slot * a.s.Hkv);
-  const SeqRows x = find_rows(a.row_begin, MODE == RowsMode::kTree ? a.tree_begin : a.seq_lens, a.rows, a.s.B, (int)slot,
-                              a.seqs_per_slot, lane, first_slot);
+  const int32_t* values = MODE == RowsMode::kTree ? a.tree_begin : a.seq_lens;
+  const SeqRows x = find_rows(a.row_begin, values, a.rows, a.s.B, (int)slot, a.seqs_per_slot, lane, first_slot);
   t.b = x.b;
   t.r0 = x.begin;
   t.n = x.end - x.begin;
@@ -242,7 +242,7 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // ---- the kernel: K and V shared through LDS ---------------------------------------------------------
 //
 // Four wavefronts of COLS columns each walk the same list of blocks, two blocks (32 tokens) a step.  The
-// step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, two steps ahead)
+// step's four 4 KiB tiles come from memory straight into LDS (each wavefront requests one, one or two steps ahead)
 // and feed the operands of all four.  A wavefront's products, for 32 columns (16: in brackets):
 //   scores  S^T[32 tok x 32 col]: 8 x v_mfma_f32_32x32x16_bf16 over the 128 dims
 //           [two of 16 tok x 16 col: 4 x v_mfma_f32_16x16x32_bf16 each]
@@ -266,9 +266,8 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // weights' computation 444, with one LDS fragment for all 498, without both 401.  32 trees of 64 nodes over 8000
 // tokens, 64 heads: 597 to 620 us.  Instructions of 16 x 16 x 32 for 32 columns: 2 % more; 64 columns a wavefront, one
 // per SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
-// 16 columns: HBM.  64 single tokens, window 4096: 176 us, 6.1 TB/s.
+// 16 columns: HBM.  64 single tokens, window 4096: 168 us, 6.4 TB/s.
 constexpr int kTileBytes = kTileElems * 2;
-constexpr int kRing = 3;  // steps in LDS: one in use, two on their way
 constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
 constexpr int kVStep = 2 * kTileBytes;
 constexpr int kStep = kKStep + kVStep;          // K, then V
@@ -301,15 +300,21 @@ struct No {
   static constexpr bool value = false;
 };
 
-// Workgroups on a CU: the rings of three fill its LDS.  The three terms of 32 columns' weights take too many registers.
+// Steps in LDS, one in use, the others on their way, and the workgroups whose rings fill a CU's LDS.  With 16 columns,
+// where the start of many short lists counts, four workgroups of a ring of 2 (2048 single tokens, window 64: 173 us,
+// three of 3: 203; 24 ragged drafts 71, 76); with 32, three of 3, but the three terms of an fp32 result's weights take
+// the registers of one.
+template <int COLS>
+constexpr int kRingSteps = COLS == 16 ? 2 : 3;
 template <bool BF16, int COLS>
-constexpr int kWavesPerSimd = BF16 || COLS == 16 ? 3 : 2;
+constexpr int kWavesPerSimd = COLS == 16 ? 4 : BF16 ? 3 : 2;
 
 template <RowsMode MODE, bool BF16, int COLS>
 __global__ __launch_bounds__(64 * W)
 __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<BF16, COLS>, kWavesPerSimd<BF16, COLS>)))
 void rows_attn_kernel(RowsAttnArgs a) {
   constexpr bool kWide = COLS == 32;
+  constexpr int kRing = kRingSteps<COLS>;
   constexpr int CT = COLS * W;          // columns of a workgroup
   constexpr int kLoads = 4;             // requests of a wavefront and step, 1 KiB each
   constexpr int kTerms = BF16 ? 1 : 3;  // bf16 parts of a weight

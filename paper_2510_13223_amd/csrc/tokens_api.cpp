@@ -33,6 +33,7 @@ constexpr int kMaxChunks = 128;
 constexpr int kMinChunkSteps = 2;
 constexpr double kStepLatencyUs = 0.7;                   // of the planner's estimate (plan_rows)
 constexpr double kStartSteps = 1.5;                      // a workgroup's start, in steps
+constexpr double kRoundUs = 3;                           // a round of workgroups behind the first
 constexpr double kMergeUs = 4;
 constexpr double kPartBytesPerUs = 4e6;
 constexpr int kRowsTileRows = 128;                       // rows of a tile at most (a group of 1)
@@ -88,17 +89,17 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
 
 // How a call's tiles are cut.  A tile is 128 columns (rows x heads of a group), or 64 where sequences have no more
 // on the mean: four wavefronts of 16 columns then share what two of 32 would do one after the other (24 drafts of
-// 13 nodes, groups of 4, fp32: 108 -> 80 us), and the loads go past the caches, as no other tile reads them.
+// 13 nodes, groups of 4, fp32: 106 -> 71 us), and the loads go past the caches, as no other tile reads them.
 //
 // A tile's list of steps (32 tokens) is cut into chunks where that is estimated to be faster.  With n
 // workgroups at work, of at most `slots`, a step takes max(latency, n x step_us): alone it is bound by the chain of
 // its products, all together by HBM or the matrix and vector units.  Each workgroup's start costs it
-// kStartSteps more; the last chunks run on while the GPU empties, a quarter of a chunk's latency on the mean; each
-// chunk's partial rows are written and read once more, after a launch.  Times in us, measured on MI355X (step_us is
-// the whole call's time per step, here in ns):
+// kStartSteps more, a round of them behind the first kRoundUs; the last chunks run on while the GPU empties, a
+// quarter of a chunk's latency on the mean; each chunk's partial rows are written and read once more, after a launch.
+// Times in us, measured on MI355X (step_us is the whole call's time per step, here in ns):
 //   64 columns, bf16 / fp32:  2.5 / 2.7     128 columns, bf16 / fp32:  2.2 / 4.4     latency of a step 0.7
-// Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.9; 64 rows, window 4096, 199
-// -> 176; 1 row over 16000 tokens 211 -> 19; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750
+// Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.8; 64 rows, window 4096, 178
+// -> 168; 1 row over 16000 tokens 211 -> 18.5; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750
 // rows, window 512, stay whole (46, in two chunks 83).
 struct RowsPlan {
   int nc = 1;
@@ -119,7 +120,7 @@ RowsPlan plan_rows(const bana_dims* d, int64_t rows, int64_t tokens, bool bf16) 
   const int64_t mean = d->total_range_tokens > 0
                            ? std::min<int64_t>(steps, d->total_range_tokens / d->batch / bana::kRowsStep + 1)
                            : steps;
-  const double slots = bf16 || thin ? 768 : 512;
+  const double slots = thin ? 1024 : bf16 ? 768 : 512;
   const double step_us = (thin ? (bf16 ? 2.5 : 2.7) : bf16 ? 2.2 : 4.4) * 1e-3;
   const double part_us = (double)rows * d->num_q_heads * 2 * (kHeadDim + 1) * sizeof(float) / kPartBytesPerUs;
   double best = 0;
@@ -129,7 +130,8 @@ RowsPlan plan_rows(const bana_dims* d, int64_t rows, int64_t tokens, bool bf16) 
     const double used = mean < steps ? std::min<double>(nc, (double)mean / chunk + 0.5) : nc;  // chunks of a tile
     const double busy = std::min(slots, std::max(groups * used, 1.0));
     const double one = (chunk + kStartSteps) * std::max(kStepLatencyUs, step_us * busy);
-    const double all = groups * (mean + used * kStartSteps) * step_us + 0.25 * chunk * kStepLatencyUs;
+    const double all = groups * (mean + used * kStartSteps) * step_us + 0.25 * chunk * kStepLatencyUs +
+                       kRoundUs * std::max(groups * used / slots - 1, 0.0);
     const double time = std::max(one, all) + (nc > 1 ? kMergeUs + used * part_us : 0);
     if (nc == 1 || time < best) {
       best = time;
