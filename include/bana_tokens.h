@@ -45,9 +45,9 @@ extern "C" {
  * this call's cache (another partition has them), rows see the ranges only.  Scores and sums are fp32; with
  * an fp32 result the weights enter the product with the values to 24 bits, with a bf16 result rounded to
  * bf16.  The fp32 result and lse of several calls over disjoint tokens merge exactly with
- * bana_merge_partials (batch = rows).  A NaN among a row's scores makes the row NaN; a row whose scores are
- * all -inf gives 0 and -inf as one that sees nothing does.  Values that a row does not see never reach it,
- * whatever they hold.
+ * bana_merge_partials (batch = rows).  A NaN or +inf among a row's scores makes the row NaN; a row whose
+ * scores are all -inf gives 0 and -inf as one that sees nothing does.  What a row does not see never
+ * reaches it, whatever its keys and values hold.
  *   q           bf16 [rows][num_q_heads][128]
  *   kv_range_*  int32 [n_parts][batch], 1 <= n_parts <= 63
  *   tree_begin  int32 [batch]
