@@ -104,7 +104,7 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 //    each for 8 dims, each read once) pass through LDS, kParts at a time; a lane then gathers 8 places of one dim
 //    and writes them with one store.
 // HBM-bound where every place moves.  Measured on MI355X: 6 sequences of 9000 tokens, every second one kept, 8 kv
-// heads: 86 us for 331 MB (blocks are read whole; 221 MB are kept tokens read and written), 3.9 TB/s.  A workgroup
+// heads: 80 us for 331 MB (blocks are read whole; 221 MB are kept tokens read and written), 4.2 TB/s.  A workgroup
 // for each (sequence, kv head), as below, took 490.
 //
 // Few kept tokens leave most of these lanes idle: 48 sequences that keep up to 7 of 48 take 7.1 us here, 4.5 in the
@@ -112,7 +112,7 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 constexpr int kFewKept = 64;  // up to here the kernel for few tokens
 
 // Wavefronts of a workgroup: 8 where that leaves at most one workgroup to a CU (1 sequence of 30000 tokens, half
-// kept: 83 us, with 4 99), else 4, three of which fit on a CU (6 of 9000: 86, with 8 164).
+// kept: 73 us, with 4 78), else 4, three of which fit on a CU (6 of 9000: 80, with 8 94; four on a CU 95).
 constexpr unsigned kFewGroups = 256;
 constexpr int kKeyUnroll = 4;
 constexpr int kPlaces = 128;  // of a wavefront's V step
@@ -175,9 +175,8 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
   constexpr int U = kPlaces / 64;
   constexpr int kStep = kPlaces * W;
   __shared__ __attribute__((aligned(16))) uint16_t sm_parts[W][kParts * 128];  // [block][8 dims][16 tokens]
-  __shared__ __attribute__((aligned(16))) uint16_t sm_froms[W][kPlaces];  // 16 x block's number + slot
+  __shared__ __attribute__((aligned(16))) uint16_t sm_froms[W][kPlaces];  // 256 x block's number + 2 x slot
   __shared__ int32_t sm_blocks[W][kPlaces];                               // pool block of each number
-  constexpr uint16_t kNone = 0xFFFF;                                                  // no source
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = lane >> 3, h = lane & 7;
   uint16_t* sm_part = sm_parts[wave];
   uint16_t* sm_from = sm_froms[wave];
@@ -205,31 +204,25 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
   look_up(wave * kPlaces);
   for (int step = 0; step < places; step += kStep) {
     const int base = step + wave * kPlaces;
-    // Number the source blocks: a place opens a new one where its block is not that of the place before.
+    // Number the source blocks: a place opens a new one where its block is not that of the place with a source before.
     int count = 0, last = -1;
     bool moves = false;
+    unsigned have[U];  // which of this lane's 8 places have a source
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int own = from_blk[u] >= 0 ? x[u] : -1;
       moves |= own > base + 64 * u + lane - shift;
-      // Places without a source take the block of the ones before them.
-      int before = own;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(before, off);
-        if (lane >= off && before < 0) before = y;
-      }
-      if (before < 0) before = last;
-      int prev = __shfl_up(before, 1);
-      if (lane == 0) prev = last;
-      const int64_t logical = (t0 + before) >> 4, logical_prev = (t0 + prev) >> 4;
-      const bool opens = own >= 0 && (prev < 0 || logical != logical_prev);
+      const uint64_t valid = __ballot(own >= 0), below = valid & ((uint64_t{1} << lane) - 1);
+      const int y = __shfl(own, below != 0 ? 63 - __clzll(below) : 0);
+      const int prev = below != 0 ? y : last;  // of the place before that has a source
+      const bool opens = own >= 0 && (prev < 0 || (t0 + own) >> 4 != (t0 + prev) >> 4);
       const uint64_t mask = __ballot(opens);
       const int number = count + __popcll(mask & ((2ull << lane) - 1)) - 1;
-      sm_from[64 * u + lane] = own >= 0 ? (uint16_t)(number * kBlockSize + (int)((t0 + own) & 15)) : kNone;
+      sm_from[64 * u + lane] = own >= 0 ? (uint16_t)(number * 256 + 2 * (int)((t0 + own) & 15)) : (uint16_t)0;
+      have[u] = (unsigned)(valid >> (8 * h)) & 0xFFu;
       if (opens) sm_block[number] = from_blk[u];
       count += (int)__popcll(mask);
-      last = __shfl(before, 63);
+      if (valid != 0) last = __builtin_amdgcn_readlane(own, 63 - __clzll(valid));
     }
     const bool any = __any(moves);
     race_check_delay(wave);
@@ -260,15 +253,23 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
         if (4 * q < m && d < m) *reinterpret_cast<u32x4*>(sm_part + d * 128 + (lane & 15) * 8) = y[q];
       }
       wave_lds_fence();
+      const char* mine = reinterpret_cast<const char*>(sm_part) + e * kBlockSize * 2;
+      if (count <= kParts) {
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int number = (from[u][j] >> 4) - part;
-          const bool here = (number >= 0) & (number < m);
-          const uint16_t y = sm_part[(here ? number : 0) * 128 + e * kBlockSize + (from[u][j] & 15)];
-          val[u][j] = here ? y : val[u][j];
-        }
+          for (int j = 0; j < 8; ++j) val[u][j] = *reinterpret_cast<const uint16_t*>(mine + from[u][j]);
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const unsigned at = (unsigned)from[u][j] - 256u * part;
+            const bool here = at < 256u * m;
+            const uint16_t x = *reinterpret_cast<const uint16_t*>(mine + (here ? at : 0u));
+            val[u][j] = here ? x : val[u][j];
+          }
+      }
       wave_lds_fence();
     }
     look_up(base + kStep);
@@ -278,15 +279,12 @@ __device__ __forceinline__ void compact_values(uint16_t* __restrict__ v, const i
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         if (to[u] < 0) continue;
-        bool all = true;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) all &= from[u][j] != kNone;
-        if (all) {
+        if (have[u] == 0xFFu) {
           *reinterpret_cast<u16x8*>(v + to[u]) = val[u];
         } else {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (from[u][j] != kNone) v[to[u] + j] = val[u][j];
+            if (have[u] >> j & 1) v[to[u] + j] = val[u][j];
         }
       }
     }
@@ -299,12 +297,15 @@ __global__ __launch_bounds__(64 * W) void compact_kernel(uint16_t* __restrict__ 
                                                          const int32_t* __restrict__ first,
                                                          const int32_t* __restrict__ kept, int max_kept,
                                                          const int32_t* __restrict__ n_kept, CacheShape s) {
-  const int part = (int)(blockIdx.x & 31), pair = (int)(blockIdx.x >> 5);  // 16 K chunks, then 16 groups of V dims
+  // The K chunks of all pairs, then the groups of V dims: mixed, they take 87 us where this takes 80.
+  const int pairs = (int)(gridDim.x >> 5), x = (int)(blockIdx.x >> 4), part = (int)(blockIdx.x & 15);
+  const bool values = x >= pairs;
+  const int pair = values ? x - pairs : x;
   const int b = pair / s.Hkv, g = pair - b * s.Hkv;
   const int n = min(max(n_kept[b], 0), max_kept);
   const int32_t* list = kept + (int64_t)b * max_kept;
-  if (part < 16) compact_keys<W>(k, table, list, n, first[b], b, g, part, s);
-  else compact_values<W>(v, table, list, n, first[b], b, g, part - 16, s);
+  if (values) compact_values<W>(v, table, list, n, first[b], b, g, part, s);
+  else compact_keys<W>(k, table, list, n, first[b], b, g, part, s);
 }
 
 // Few tokens: one workgroup per (sequence, kv head), 16 kept tokens at a time, a thread for each token and 8 dims.
