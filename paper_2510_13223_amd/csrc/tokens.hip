@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "packed_rows.h"
 #include "paged_addr.h"
 #include "tokens.h"
@@ -107,9 +109,11 @@ __global__ __launch_bounds__(256) void append_kernel(const uint16_t* __restrict_
 // heads: 80 us for 331 MB (blocks are read whole; 221 MB are kept tokens read and written), 4.2 TB/s.  A workgroup
 // for each (sequence, kv head), as below, took 490.
 //
-// Few kept tokens leave most of these lanes idle: 48 sequences that keep up to 7 of 48 take 7.1 us here, 4.5 in the
-// kernel below, which reads V element by element but has all of a token's dims under way at once.
-constexpr int kFewKept = 64;  // up to here the kernel for few tokens
+// Few kept tokens leave most of these lanes idle, and their 32 workgroups per pair start for nothing.  The kernel below
+// has one, which walks 16 tokens at a time and reads V element by element: faster up to a length that grows with the
+// number of pairs.  us, below / here: 384 pairs 7 kept 4.4 / 35, 126 kept 20 / 41, 252 kept 37 / 44, 504 kept 91 / 59;
+// 48 pairs 63 kept 6.1 / 6.8, 126 kept 10 / 7.0; 8 pairs 63 kept 5.8 / 4.7.
+inline int few_kept(unsigned pairs) { return (int)std::min(32 + pairs / 4 * 3, 256u); }
 
 // Wavefronts of a workgroup: 8 where that leaves at most one workgroup to a CU (1 sequence of 30000 tokens, half
 // kept: 73 us, with 4 78), else 4, three of which fit on a CU (6 of 9000: 80, with 8 94; four on a CU 95).
@@ -369,7 +373,7 @@ hipError_t launch_append(const void* k_rows, const void* v_rows, int rows, const
 hipError_t launch_compact(void* k, void* v, const int32_t* table, const int32_t* first, const int32_t* kept,
                           int max_kept, const int32_t* n_kept, CacheShape s, hipStream_t stream) {
   const unsigned pairs = (unsigned)s.B * (unsigned)s.Hkv;
-  if (max_kept <= kFewKept)
+  if (max_kept <= few_kept(pairs))
     hipLaunchKernelGGL(compact_few_kernel, dim3(pairs), dim3(256), 0, stream, static_cast<uint16_t*>(k),
                        static_cast<uint16_t*>(v), table, first, kept, max_kept, n_kept, s);
   else if (pairs * 32u <= kFewGroups)

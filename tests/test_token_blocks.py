@@ -59,7 +59,7 @@ def test_append_skips_tokens_without_a_block():
     (1, [9000, 700], [13, 1], 0.03), (2, [2111, 0, 640, 90], [3, 0, 8, 0], 0.97), (1, [300], [7], 0.25),
     (1, [1100, 1100], [0, 7], 1.0),
     (8, [2111, 0, 640, 90], [3, 0, 8, 0], 0.97), (4, [3000, 1, 700], [5, 0, 15], 0.6), (12, [5000], [1], 0.04),
-    (5, [1100, 1100], [0, 7], 1.0),
+    (5, [1100, 1100], [0, 7], 1.0), (40, [400, 300, 90], [0, 5, 7], 0.25), (40, [400, 300, 90], [0, 5, 7], 0.5),
 ])
 def test_compact(hkv, lens, first, keep):
     rng = random.Random(7)
