@@ -48,21 +48,47 @@ struct Tile {
   bool any;             // some column exists
 };
 
+// Where sequences have a few tiles or less and one load sees them all, their tiles are counted, so that those that
+// exist are numbered without gaps.  (The numbering by floor(row_begin[b] G / CT) + b leaves one behind every sequence
+// whose columns fill its tiles, and workgroups that end at once every so often leave some CUs without work.)
+// 24 trees of 32 nodes, groups of 4, by that numbering / counted: fp32 165 / 124 us, bf16 119 / 102; a count costs
+// up to 0.8 us.
 template <RowsMode MODE, int CT>
 __device__ __forceinline__ Tile find_tile(const RowsAttnArgs& a, unsigned wg, int lane) {
   const unsigned slot = a.by_hkv.quotient(wg);
-  auto first_slot = [&](int b, int row) { return row * a.G / CT + b; };
+  const int B = a.s.B;
+  const int32_t* values = MODE == RowsMode::kTree ? a.tree_begin : a.seq_lens;
   Tile t;
   t.g = (int)(wg - slot * a.s.Hkv);
-  const int32_t* values = MODE == RowsMode::kTree ? a.tree_begin : a.seq_lens;
-  const SeqRows x = find_rows(a.row_begin, values, a.rows, a.s.B, (int)slot, a.seqs_per_slot, lane, first_slot);
-  t.b = x.b;
-  t.r0 = x.begin;
-  t.n = x.end - x.begin;
-  const int span = a.s.max_blocks * kBlockSize;
-  t.tokens = MODE == RowsMode::kTree ? min(x.value, span) : min(max(x.value, 0), span);
-  t.c0 = ((int)slot - first_slot(x.b, x.begin)) * CT;
+  int value;
+  if (a.count_tiles) {  // B <= 64: a sequence per lane
+    const int start = row_start(a.row_begin, min(lane, B), a.rows), its = values[min(lane, B - 1)];
+    const int n = row_start(a.row_begin, min(lane + 1, B), a.rows) - start;
+    const int tiles = (max(n, 0) * a.G + CT - 1) / CT;
+    int past = tiles;  // tiles of the sequences up to this one
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) {
+      const int y = __shfl_up(past, off);
+      if (lane >= off) past += y;
+    }
+    const uint64_t behind = __ballot(past > (int)slot);
+    t.b = behind != 0 ? __ffsll((unsigned long long)behind) - 1 : 0;  // past the last tile: c0 is outside
+    t.r0 = __builtin_amdgcn_readlane(start, t.b);
+    t.n = __builtin_amdgcn_readlane(n, t.b);
+    value = __builtin_amdgcn_readlane(its, t.b);
+    t.c0 = behind != 0 ? ((int)slot - __builtin_amdgcn_readlane(past - tiles, t.b)) * CT : -1;
+  } else {
+    auto first_slot = [&](int b, int row) { return row * a.G / CT + b; };
+    const SeqRows x = find_rows(a.row_begin, values, a.rows, B, (int)slot, a.seqs_per_slot, lane, first_slot);
+    t.b = x.b;
+    t.r0 = x.begin;
+    t.n = x.end - x.begin;
+    value = x.value;
+    t.c0 = ((int)slot - first_slot(x.b, x.begin)) * CT;
+  }
   t.any = t.c0 >= 0 && t.c0 < t.n * a.G;
+  const int span = a.s.max_blocks * kBlockSize;
+  t.tokens = MODE == RowsMode::kTree ? min(value, span) : min(max(value, 0), span);
   return t;
 }
 
@@ -718,6 +744,8 @@ hipError_t launch_rows_attn(const RowsAttnArgs& args, RowsMode mode, bool bf16, 
   const int64_t slots = (int64_t)a.rows * a.G / a.tile + a.s.B;
   a.tiles = (unsigned)slots * (unsigned)a.s.Hkv;
   a.seqs_per_slot = (float)a.s.B / (float)slots;
+  a.count_tiles = a.s.B > 1 && a.s.B <= 64 && (int64_t)a.rows * a.G * 4 >= (int64_t)a.tile * a.s.B &&
+                  (int64_t)a.rows * a.G < (int64_t)a.tile * a.s.B * 8;
   a.by_tiles.set(a.tiles);
   if (mode == RowsMode::kTree) {
     if (bf16) launch_tiles<RowsMode::kTree, true>(a, stream);

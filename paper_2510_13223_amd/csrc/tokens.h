@@ -44,6 +44,7 @@ struct RowsAttnArgs {
   // Set by the launcher:
   unsigned tiles;       // workgroups of a chunk
   float seqs_per_slot;  // sequences per tile of a kv head
+  bool count_tiles;     // number the tiles by counting them, not by their sequence's first row
   FastDiv by_tiles;
 };
 

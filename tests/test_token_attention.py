@@ -85,6 +85,10 @@ TREES = [
     (8, 1, [50], [70], 1),                              # more than 64 rows: the nodes behind 64 are not seen
     (12, 4, [1, 2, 3, 40, 5, 90, 7, 8, 9], [2, 1, 0, 12, 1, 1, 0, 6, 2], 2),
     (16, 4, [900, 30], [20, 40], 4),
+    (8, 2, [40, 50, 60], [32, 32, 32], 1),              # tiles filled to the last column
+    (8, 2, [40, 5, 60, 7, 9], [0, 16, 0, 16, 0], 1),
+    (4, 2, [3] * 64, [5] * 64, 1),                      # as many sequences as lanes, and one more
+    (4, 2, [3] * 65, [20] * 65, 1),
 ]
 
 
