@@ -301,12 +301,14 @@ constexpr float kSlack = 8.f;
 constexpr int W = 4;  // wavefronts of a workgroup
 static_assert(32 * W == kRowsTile, "the planner's tile");
 
-// 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.  STREAM: read by
-// this workgroup only, past the caches.
+// 4 KiB from memory into LDS: lane l's 16 bytes at base + offset[x] go to lds + 1024 x + 16 l.  STREAM: past the caches.
+// base may have been read from a lane just before, and a memory instruction must not read a scalar register within 5
+// wait states of the vector instruction that wrote it; nobody counts them into inline assembly, so it has them itself:
+// one of the move, four of the s_nop.  (Setting m0 takes one more only before a load that uses it.)
 #pragma clang diagnostic ignored "-Winline-asm"  // m0 as a clobber: nothing else here uses it
 #define FETCH_4K(hint)                                                                                        \
   asm volatile(                                                                                               \
-      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %5" hint                                   \
+      "s_mov_b32 m0, %4\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %5" hint                                   \
       "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %5" hint                      \
       "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %5" hint                      \
       "\n\ts_add_u32 m0, m0, 0x400\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %5" hint ::"v"(offset[0]),    \
