@@ -344,7 +344,8 @@ __global__ __launch_bounds__(256) void compact_few_kernel(uint16_t* __restrict__
 #pragma unroll
       for (int e = 0; e < 8; ++e) val[e] = v[tile + (8 * ch + e) * kBlockSize + slot];
     }
-    __syncthreads();  // everything of the step is read
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // what this wavefront reads has arrived
+    __syncthreads();
     if (move) {
       const int64_t tile = kv_tile(to, g, s.Hkv) * kTileElems;
       const int slot = (int)((t0 + base + i) & 15);

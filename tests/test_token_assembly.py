@@ -1,5 +1,5 @@
 """The compiled kernels of the calls on new tokens (assembly of this repository's own sources, made here), read for the
-waits that the compiler does not place by itself."""
+waits that the compiler does not place by itself: around inline assembly, and before a barrier that orders memory."""
 
 import os
 import re
@@ -88,3 +88,24 @@ def test_memory_instructions_wait_for_scalars_that_vector_instructions_wrote(ker
                 assert not scalars_written(lines[p]) & reads, f"{name}: {lines[p]!r} {waited} before {line!r}"
                 todo += [(q, waited + wait_states(lines[p])) for q in before[p]]
     assert seen > 0
+
+
+def test_in_place_moves_have_read_before_the_barrier(kernels):
+    """Compaction in place: at the barrier between a step's reads and its writes, every wavefront's own loads have
+    arrived, on every path back from the barrier to them."""
+    found = [n for n in kernels if "compact" in n]
+    for name in found:
+        lines = kernels[name]
+        before = predecessors(lines)
+        barriers = [i for i, line in enumerate(lines) if line.startswith("s_barrier")]
+        assert barriers
+        for i in barriers:
+            todo, done = list(before[i]), set()
+            while todo:
+                p = todo.pop()
+                if p in done or re.match(r"s_waitcnt.*vmcnt\(0\)", lines[p]):
+                    continue
+                done.add(p)
+                assert not lines[p].startswith("global_load"), f"{name}: {lines[p]!r} may be under way at the barrier"
+                todo += before[p]
+    assert found or not any("append" in n for n in kernels)
