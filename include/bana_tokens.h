@@ -120,7 +120,7 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
  *      whose first table entry is not -1                (fork: the call changed nothing else)
  *   3  a table too short for the tokens asked for       (reserve: the call changed nothing else)
  *   4  a table entry that names no block of the pool, or whose block has no reference left
- *      (release: the entry is cleared; fork: it is copied, its block left alone)
+ *      (release: the entry is cleared; fork: see there)
  * All results are the same from run to run.  These calls change one table: they must not overlap.
  * workspace (bana_kv_blocks_workspace_bytes bytes, needed): not shared by calls that may overlap.
  *
@@ -131,7 +131,9 @@ bana_status bana_compact_kv_tokens(const bana_dims* d, void* k_cache, void* v_ca
  * src_seq[i]: its whole blocks are shared (counts + 1), a last block that is only partly filled is copied
  * into the free block of the lowest number left, in the order of i (count 1),
  * seq_lens[dst_seq[i]] = seq_lens[src_seq[i]] (clamped to the table's span).  One source may have several
- * destinations.
+ * destinations.  An entry of a source that names no block of the pool, or one without references: a whole block's is
+ * copied and its count left alone; a partly filled one's tokens are copied if there are any (the destination has its
+ * free block in any case); a block without references that a source names is no free block of this call.  Status 4.
  * bana_release_kv_blocks: for every sequence the entries from ceil(keep_lens[b] / 16) on are given back:
  * count - 1, entry -1 (keep_lens[b] <= 0: all of them; beyond the table: none).
  * Of d, num_q_heads is not used; nor are the heads in reserve and release.  BANA_ERR_UNSUPPORTED:

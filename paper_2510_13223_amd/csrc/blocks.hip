@@ -7,7 +7,7 @@
 //
 // Bound by the latency of dependent reads, not by their bytes: lengths, table entries, counts, list, each a round trip
 // of some 0.7 us, and two launches for a fork.  Measured on MI355X: blocks for 128 drafts of 64 tokens, pool of
-// 116,000, 8.6 us; 96 forks of 1500 tokens, 8 kv heads, 12.4 us.
+// 116,000, 8.6 us; 96 forks of 1500 tokens, 8 kv heads, and their release, 15.6 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -86,8 +86,9 @@ __device__ __forceinline__ int64_t find_free(const int32_t* __restrict__ refs, i
   return found;
 }
 
-// Workspace: [0] 1 if the plan holds, [2..] 64-bit need; [64, 64 + B) counts or marks, [64 + B, 64 + 2 B) prefix
-// sums, then the list of blocks.
+// Workspace: reserve has prefix sums in [64, 64 + B) and the list of blocks from 64 + 2 B on.  Fork: [0] 1 if the plan
+// holds, [1] 1 if a source names a block without references, [64, 64 + B) marks, then places in the list, [64 + B,
+// 64 + 2 B) the list, then the blocks kept from the search.
 __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(int32_t* __restrict__ table,
                                                                const int32_t* __restrict__ lens,
                                                                const int32_t* __restrict__ need,
@@ -152,27 +153,108 @@ __device__ __forceinline__ int64_t length_of(const int32_t* __restrict__ lens, i
   return min((int64_t)max(lens[b], 0), (int64_t)s.max_blocks * kBlockSize);
 }
 
+// One fork of a call, its indices in order (else valid is false).
+struct Fork {
+  int src, dst;
+  int64_t len;  // of the source
+  bool valid;
+};
+
+__device__ __forceinline__ Fork fork_at(const int32_t* __restrict__ src, const int32_t* __restrict__ dst, int i,
+                                        const int32_t* __restrict__ table, const int32_t* __restrict__ lens,
+                                        const CacheShape& s) {
+  const int a = src[i], d = dst[i];
+  const bool inside = a >= 0 && a < s.B && d >= 0 && d < s.B;
+  const int64_t len = length_of(lens, inside ? a : 0, s);
+  return {a, d, len, inside && table[(int64_t)(inside ? d : 0) * s.max_blocks] == -1};
+}
+
+// f(block, named) for every entry of the sources of the forks i that are chosen(i, fork): whether it names a block of the
+// pool, and which (else some block of it).  fork(i) is fork i.  A thread takes a piece of a source's entries, so that
+// those of 1024 forks are under way together.  Every thread calls it.
+constexpr int kPiece = 4;
+
+template <typename G, typename C, typename F>
+__device__ __forceinline__ void for_source_blocks(int n, G fork, const int32_t* __restrict__ table,
+                                                  const CacheShape& s, int* sm, C chosen, F f) {
+  typedef int32_t i32x4 __attribute__((ext_vector_type(4), aligned(4)));
+  __shared__ int sm_seq[kPlanThreads], sm_entries[kPlanThreads], sm_first[kPlanThreads];
+  int half = 1;  // of the forks looked at together, a power of two
+  while (2 * half < min(n, kPlanThreads)) half *= 2;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + threadIdx.x;
+    int seq = 0, entries = 0;
+    if (i < n) {
+      const Fork x = fork(i);
+      seq = x.src;
+      if (chosen(i, x)) entries = blocks_of(x.len);
+    }
+    int pieces;
+    const int first = block_scan((entries + kPiece - 1) / kPiece, sm, &pieces);
+    race_check_delay(threadIdx.x >> 6);
+    sm_seq[threadIdx.x] = seq, sm_entries[threadIdx.x] = entries, sm_first[threadIdx.x] = first;
+    __syncthreads();
+    race_check_barrier();
+    for (int x = threadIdx.x; x < pieces; x += kPlanThreads) {
+      int k = 0;  // the last fork whose pieces start at x or before
+      for (int step = half; step >= 1; step /= 2)
+        if (sm_first[k + step] <= x) k += step;
+      const int32_t* row = table + (int64_t)sm_seq[k] * s.max_blocks;
+      const int j = (x - sm_first[k]) * kPiece, end = sm_entries[k];
+      i32x4 blk[kPiece / 4];
+      if (j + kPiece <= s.max_blocks) {
+#pragma unroll
+        for (int q = 0; q < kPiece / 4; ++q) blk[q] = *reinterpret_cast<const i32x4*>(row + j + 4 * q);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kPiece; ++e) blk[e >> 2][e & 3] = row[min(j + e, end - 1)];
+      }
+#pragma unroll
+      for (int e = 0; e < kPiece; ++e) {
+        const int y = blk[e >> 2][e & 3];
+        f(min(max(y, 0), s.last_block), (j + e < end) & (y >= 0) & (y <= s.last_block));
+      }
+    }
+  }
+}
+
+// The counts of the blocks that the sources name are judged before any changes: one without references is left alone by
+// the forks (ws[1] tells them to look; looking always would cost the next kernel 9 us, as loads of the counts then meet
+// the atomics on them) and is no free block of this call, whatever its count.  96 forks of 32 sequences of 1500 tokens:
+// 8.8 us, without the walk over the sources' entries 5.4; with 16 entries to a thread 9.4, most of that more code to fetch.
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const int32_t* __restrict__ src,
                                                                  const int32_t* __restrict__ dst, int n,
                                                                  const int32_t* __restrict__ table,
-                                                                 const int32_t* __restrict__ lens,
-                                                                 int32_t* __restrict__ refs, int64_t num_blocks,
-                                                                 int32_t* __restrict__ status,
+                                                                 const int32_t* __restrict__ lens, int32_t* refs,
+                                                                 int64_t num_blocks, int32_t* __restrict__ status,
                                                                  int32_t* __restrict__ ws, CacheShape s) {
-  __shared__ int sm[kPlanWaves];
-  int32_t* mark = ws + 64;            // [B]: 1 + the fork that writes the sequence, 0: none
-  int32_t* list = ws + 64 + s.B;      // [min(n, B)] block of each fork that takes one, in order
+  __shared__ int sm[kPlanWaves], sm_held;
+  int32_t* mark = ws + 64;        // [B]: 0 none, 1 a destination, 2 + i the source of fork i (the last of them)
+  int32_t* list = ws + 64 + s.B;  // [min(n, B)] block of each fork that takes one, in order
+  int32_t* held = list + s.B;     // [min(entries, num_blocks)] blocks kept from the search
+  const int own_i = threadIdx.x;
+  Fork own = {};
+  if (own_i < n) own = fork_at(src, dst, own_i, table, lens, s);
+  auto fork = [&](int i) { return i == own_i ? own : fork_at(src, dst, i, table, lens, s); };
   for (int b = threadIdx.x; b < s.B; b += kPlanThreads) mark[b] = 0;
+  if (threadIdx.x == 0) sm_held = 0;
   __syncthreads();
   bool bad = n > s.B;
-  for (int i = threadIdx.x; i < n && !bad; i += kPlanThreads) {
-    const int d = dst[i], c = src[i];
-    bad = d < 0 || d >= s.B || c < 0 || c >= s.B || table[(int64_t)d * s.max_blocks] != -1 ||
-          atomicExch(mark + d, 1) != 0;
+  for (int i = own_i; i < n && !bad; i += kPlanThreads) {
+    const Fork x = fork(i);
+    bad = !x.valid || atomicExch(mark + x.dst, 1) != 0;
   }
+  const bool valid = !bad;
   __syncthreads();
-  for (int i = threadIdx.x; i < n && !bad; i += kPlanThreads)
-    bad = __hip_atomic_load(mark + src[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) != 0;
+  bool odd = false;
+  for_source_blocks(
+      n, fork, table, s, sm,
+      [&](int i, const Fork& x) {
+        const int before = valid ? atomicMax(mark + x.src, 2 + i) : 1;
+        bad |= before == 1;
+        return before == 0;
+      },
+      [&](int blk, bool named) { odd |= named & (refs[blk] <= 0); });
   if (__syncthreads_or(bad)) {
     if (threadIdx.x == 0) {
       atomicMax(status, 2);
@@ -180,15 +262,30 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const int32_t* 
     }
     return;
   }
+  odd = __syncthreads_or(odd);
+  if (odd) {  // rare, and wrong of the caller: counts of 0 are marked until the search is over
+    for_source_blocks(
+        n, fork, table, s, sm,
+        [&](int i, const Fork& x) {
+          return __hip_atomic_load(mark + x.src, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 2 + i;
+        },
+        [&](int blk, bool named) {
+          if (named && atomicCAS(refs + blk, 0, INT32_MIN) == 0) held[atomicAdd(&sm_held, 1)] = blk;
+        });
+    __syncthreads();
+    __threadfence();  // the search reads around the atomics
+  }
   int64_t total = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + threadIdx.x;
     int sum;
-    const int at = block_scan(i < n && length_of(lens, src[i], s) % kBlockSize != 0, sm, &sum);
+    const int at = block_scan(i < n && fork(i).len % kBlockSize != 0, sm, &sum);
     if (i < n) mark[i] = (int32_t)(total + at);  // place in the list (the marks are done with)
     total += sum;
   }
   const int64_t found = total > num_blocks ? 0 : find_free(refs, num_blocks, total, list, sm);
+  __syncthreads();
+  for (int x = threadIdx.x; x < sm_held; x += kPlanThreads) refs[held[x]] = 0;
   if (found < total) {
     if (threadIdx.x == 0) {
       atomicMax(status, 1);
@@ -196,9 +293,8 @@ __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const int32_t* 
     }
     return;
   }
-  __syncthreads();
   for (int64_t i = threadIdx.x; i < total; i += kPlanThreads) refs[list[i]] = 1;
-  if (threadIdx.x == 0) ws[0] = 1;
+  if (threadIdx.x == 0) ws[0] = 1, ws[1] = odd;
 }
 
 // kForkParts workgroups per fork: the shared entries (the first), and the copy of the last block if it is partly
@@ -210,7 +306,8 @@ __global__ __launch_bounds__(256) void fork_kernel(const int32_t* __restrict__ s
                                                    int32_t* __restrict__ table, int32_t* __restrict__ lens,
                                                    int32_t* __restrict__ refs, int32_t* __restrict__ status,
                                                    const int32_t* __restrict__ ws, CacheShape s) {
-  if (ws[0] == 0) return;
+  const int holds = ws[0], odd = ws[1];
+  if (holds == 0) return;
   const int i = blockIdx.x / kForkParts, part = blockIdx.x % kForkParts;
   const int from = src[i], to = dst[i];
   const int64_t len = length_of(lens, from, s);
@@ -218,11 +315,15 @@ __global__ __launch_bounds__(256) void fork_kernel(const int32_t* __restrict__ s
   const int32_t* of = table + (int64_t)from * s.max_blocks;
   int32_t* entry = table + (int64_t)to * s.max_blocks;
   bool bad = false;
+  // Forks raise only counts above 0, and the plan took no block that a source names: a count keeps its sign.
+  auto counted = [&](int32_t blk) {
+    return odd == 0 || __hip_atomic_load(refs + blk, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) > 0;
+  };
   if (part == 0) {
     for (int j = threadIdx.x; j < whole; j += 256) {
       const int32_t blk = of[j];
       entry[j] = blk;
-      if (blk >= 0 && blk <= s.last_block) atomicAdd(refs + blk, 1);
+      if (blk >= 0 && blk <= s.last_block && counted(blk)) atomicAdd(refs + blk, 1);
       else bad = true;
     }
     if (threadIdx.x == 0) lens[to] = (int32_t)len;
@@ -232,6 +333,7 @@ __global__ __launch_bounds__(256) void fork_kernel(const int32_t* __restrict__ s
     const int32_t blk = of[whole];
     if (part == 0 && threadIdx.x == 0) entry[whole] = fresh;
     if (blk >= 0 && blk <= s.last_block) {
+      bad |= part == 0 && !counted(blk);
       const int64_t n16 = (int64_t)s.Hkv * kTileElems / 8;
       for (int64_t x = part * 256 + threadIdx.x; x < n16; x += 256 * kForkParts) {
         const u32x4 key = k[blk * n16 + x], val = v[blk * n16 + x];

@@ -1,0 +1,129 @@
+"""Calls on new tokens and blocks where the cache is unusual: counts and entries that do not fit together."""
+
+import pytest
+import torch
+
+import token_cases as tc
+from paper_2510_13223_amd import bana
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+def ints(x):
+    return torch.tensor(x, dtype=torch.int32, device=DEV)
+
+
+def same(x, y):
+    """Equal bit for bit (pools hold NaN)."""
+    x, y = x.cpu(), y.cpu()
+    if x.dtype == torch.bfloat16:
+        x, y = x.view(torch.int16), y.view(torch.int16)
+    return torch.equal(x, y)
+
+
+# ---- counts and entries that do not fit together ----------------------------------------------------
+
+class Blocks:
+    """A table with its counts and a pool of random tiles, on the device; `lens` tokens a sequence, one count an entry."""
+
+    def __init__(self, lens, num_blocks, width, seed):
+        g = torch.Generator().manual_seed(seed)
+        perm = torch.randperm(num_blocks, generator=g).tolist()
+        self.lens, self.status = ints(lens), ints([0])
+        self.table = torch.full((len(lens), width), -1, dtype=torch.int32)
+        self.refs = torch.zeros(num_blocks, dtype=torch.int32)
+        for b, n in enumerate(lens):
+            for j in range(tc.blocks_of(n)):
+                self.table[b, j] = perm.pop()
+                self.refs[self.table[b, j]] += 1
+        self.table, self.refs = self.table.to(DEV), self.refs.to(DEV)
+        self.k = torch.randn((num_blocks, 1, 16, 16, 8), generator=g).to(torch.bfloat16).to(DEV)
+        self.v = torch.randn((num_blocks, 1, 128, 16), generator=g).to(torch.bfloat16).to(DEV)
+        n = bana.bana_kv_blocks_workspace_bytes(len(lens), width, num_blocks)
+        self.ws = torch.full((n,), 0x7F, dtype=torch.uint8, device=DEV)
+
+    def copy(self):
+        return [x.cpu().clone() for x in (self.k, self.v, self.table, self.lens, self.refs, self.status)]
+
+
+def fork(src, dst, k, v, table, lens, refs, status):
+    """The forks of a call that is in order but for blocks without references among its sources'."""
+    width, nb = table.shape[1], len(refs)
+    length = [min(max(int(lens[s]), 0), width * tc.BS) for s in src]
+    named = {int(table[s, j]) for s, n in zip(src, length) for j in range(tc.blocks_of(n))}
+    bad = {x for x in named if not 0 <= x < nb or refs[x] <= 0}
+    free = [x for x in range(nb) if refs[x] == 0 and x not in bad]
+    if len(free) < sum(n % tc.BS != 0 for n in length):
+        status[0] = max(int(status[0]), 1)
+        return
+    if bad:
+        status[0] = 4
+    for s, d, n in zip(src, dst, length):
+        for j in range(n // tc.BS):
+            table[d, j] = table[s, j]
+            if int(table[s, j]) not in bad:
+                refs[table[s, j]] += 1
+        if n % tc.BS:
+            blk, fresh = int(table[s, n // tc.BS]), free.pop(0)
+            table[d, n // tc.BS] = fresh
+            refs[fresh] = 1
+            if 0 <= blk < nb:
+                k[fresh], v[fresh] = k[blk], v[blk]
+        lens[d] = n
+
+
+def check_fork(p, src, dst, status):
+    want = p.copy()
+    fork(src, dst, *want)
+    bana.bana_fork_kv_seqs(ints(src), ints(dst), p.k, p.v, p.table, p.lens, p.refs, p.status, p.ws)
+    for x, y, name in zip(p.copy(), want, ("k", "v", "table", "lens", "refs", "status")):
+        assert same(x, y), name
+    assert int(p.status) == status
+
+
+@pytest.mark.parametrize("count", [0, -3])
+@pytest.mark.parametrize("entry", [0, 1, 2])
+def test_fork_of_a_block_without_references(entry, count):
+    """Raised as 4: its entry is copied, its count left alone, and the block, here the one of the lowest number, is no
+    free one for this call."""
+    p = Blocks([40, 37, 0, 0, 0], 12, 4, 1)
+    other = int(p.table[0, entry])
+    p.table[p.table == 0] = other
+    p.table[0, entry] = 0  # the block's number, and another sequence's if that was it
+    p.refs.zero_()
+    p.refs[p.table[p.table >= 0].long()] = 1
+    p.refs[0] = count
+    check_fork(p, [0, 0, 1], [4, 2, 3], 4)
+
+
+def test_fork_where_only_named_blocks_look_free():
+    """Two blocks are free by their counts, and a source names one of them: too few, and nothing else changes."""
+    p = Blocks([40, 37, 0, 0], 8, 4, 2)
+    free = (p.refs == 0).nonzero().flatten().tolist()
+    p.refs[free[1]], p.refs[p.table[1, 2].long()] = 1, 0
+    before = p.copy()
+    check_fork(p, [0, 1], [2, 3], 1)
+    for x, y in zip(p.copy()[:-1], before[:-1]):
+        assert same(x, y)
+
+
+def test_many_forks_of_blocks_without_references():
+    """More forks than threads of the plan, sources named many times, one long, blocks without references in some that
+    share them."""
+    n = 1300
+    lens = [5000, 64, 7, 0, 33, 300] + [20] * 1200 + [0] * n
+    p = Blocks(lens, 6000, 320, 3)
+    for b, j in ((0, 0), (0, 250), (0, 312), (2, 0), (4, 1), (5, 18), (700, 0), (1205, 1)):
+        p.refs[p.table[b, j].long()] = 0
+    p.table[1, 2] = p.table[0, 250]  # by two sources
+    p.table[800, 0] = p.table[700, 0]
+    src = [0, 1, 2, 3, 4, 5] * 16 + list(range(6, 1206))
+    src += [0] * (n - len(src))
+    check_fork(p, src, [1206 + (7 * i) % n for i in range(n)], 4)
+
+
+def test_fork_beside_unnamed_free_blocks_is_as_before():
+    """Blocks in order: no status, the lowest free numbers."""
+    p = Blocks([40, 37, 160, 0, 0, 0, 0], 30, 10, 4)
+    check_fork(p, [0, 1, 0, 2], [3, 5, 4, 6], 0)
