@@ -111,7 +111,7 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(int32_t* __restri
 #pragma unroll
         for (int u = 0; u < 4; ++u) x[u] = table[(int64_t)b * s.max_blocks + min(j + u, end - 1)];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) count += (j + u < end) & (x[u] < 0);
+        for (int u = 0; u < 4; ++u) count += (j + u < end) & (x[u] == -1);
       }
     }
     int sum;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(kPlanThreads) void reserve_kernel(int32_t* __restri
       for (int u = 0; u < 4; ++u) fresh[u] = list[max(min((int64_t)at + u, total - 1), (int64_t)0)];
 #pragma unroll
       for (int u = 0, k = 0; u < 4; ++u) {
-        if (j + u >= end || x[u] >= 0) continue;
+        if (j + u >= end || x[u] != -1) continue;
         const int32_t blk = k == 0 ? fresh[0] : k == 1 ? fresh[1] : k == 2 ? fresh[2] : fresh[3];
         entry[u] = blk;
         refs[blk] = 1;

@@ -127,3 +127,17 @@ def test_fork_beside_unnamed_free_blocks_is_as_before():
     """Blocks in order: no status, the lowest free numbers."""
     p = Blocks([40, 37, 160, 0, 0, 0, 0], 30, 10, 4)
     check_fork(p, [0, 1, 0, 2], [3, 5, 4, 6], 0)
+
+
+def test_reserve_leaves_entries_that_are_not_minus_one():
+    """Only entries of -1 are taken for empty."""
+    p = Blocks([16, 0, 0], 20, 6, 5)
+    p.table[0, 2], p.table[1, 0], p.table[1, 3], p.table[2, 1] = -7, -2, 99, -2 ** 31
+    want = p.copy()
+    free = [x for x in range(20) if want[4][x] == 0]
+    for b, j in ((0, 1), (0, 3), (1, 1), (1, 2), (1, 4), (2, 0)):
+        want[2][b, j] = free.pop(0)
+        want[4][want[2][b, j]] = 1
+    bana.bana_reserve_kv_blocks(p.table, p.lens, ints([64, 80, 32]), p.refs, p.status, p.ws)
+    for x, y in zip(p.copy(), want):
+        assert same(x, y)
