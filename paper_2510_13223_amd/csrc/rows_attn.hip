@@ -252,10 +252,11 @@ template <bool BF16, int STRIDE>
 __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restrict__ lse, int64_t row,
                                           const f32x4 (&acc)[kHeadDim / STRIDE], float l, float m, int first) {
   const bool empty = l == 0.f;
-  const float inv = empty ? 0.f : 1.0f / l;
+  const float inv = 1.0f / l;
 #pragma unroll
   for (int j = 0; j < kHeadDim / STRIDE; ++j) {
-    const f32x4 o = acc[j] * inv;
+    // A row whose scores are all -inf has sums of NaN where values are infinite: 0 by choice, not by the product.
+    const f32x4 o = empty ? f32x4{0.f, 0.f, 0.f, 0.f} : acc[j] * inv;
     const int64_t at = row * kHeadDim + STRIDE * j + first;
     if (BF16)
       *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(out) + at) = u32x2{bf16_pair(o[0], o[1]), bf16_pair(o[2], o[3])};

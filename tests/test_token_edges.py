@@ -1,4 +1,7 @@
-"""Calls on new tokens and blocks where the cache is unusual: counts and entries that do not fit together."""
+"""Calls on new tokens and blocks where the cache is unusual: scores that are not finite, counts and entries that do not
+fit together."""
+
+import math
 
 import pytest
 import torch
@@ -20,6 +23,53 @@ def same(x, y):
     if x.dtype == torch.bfloat16:
         x, y = x.view(torch.int16), y.view(torch.int16)
     return torch.equal(x, y)
+
+
+def run(cache, q, rb, bf16, window=None, tree=None, ws=True):
+    """(out, lse) of one attention call: window = (seq_lens, window, sinks), tree = (begin, end, tree_begin, masks)."""
+    rows, hq, _ = q.shape
+    out = torch.full((rows, hq, tc.D), 7.0, dtype=torch.bfloat16 if bf16 else torch.float32, device=DEV)
+    lse = torch.full((rows, hq), 7.0, device=DEV)
+    dims = bana.make_dims(len(cache.lens), hq, cache.hkv, cache.table.shape[1], cache.num_blocks,
+                          max_range_tokens=max(cache.lens), total_range_tokens=sum(cache.lens))
+    n = (bana.bana_window_attn_workspace_bytes(dims, rows, *window[1:]) if window else
+         bana.bana_tree_attn_workspace_bytes(dims, rows, len(tree[0])))
+    w = torch.full((n,), 0xFF, dtype=torch.uint8, device=DEV) if ws and n else None
+    args = (q.to(DEV), ints(rb), cache.k.to(DEV), cache.v.to(DEV), cache.table.to(DEV))
+    more = dict(scale=0.0884, workspace=w, dims=dims)
+    if window:
+        bana.bana_window_attn(*args, ints(window[0]), *window[1:], out, lse, **more)
+    else:
+        begin, end, at, masks = tree
+        bana.bana_tree_attn(*args, ints(begin), ints(end), ints(at), tc.signed(masks).to(DEV), out, lse, **more)
+    torch.cuda.synchronize()
+    return out.cpu(), lse.cpu()
+
+
+def queries(rows, hq, seed):
+    return torch.randn((rows, hq, tc.D), generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+# ---- scores and values that are not finite ----------------------------------------------------------
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("news", [3, 60])  # tiles of 64 columns and of 128
+def test_scores_of_minus_infinity_give_zero_whatever_the_values(news, bf16, ws):
+    """A row whose scores are all -inf is as one that sees nothing, also where its values are infinite or NaN."""
+    lens = [900, 100]
+    cache = tc.Cache(lens, 2, 3)
+    cache.keys[0][:, :, 0] = -math.inf
+    cache.values[0][:, :, 5], cache.values[0][:, 1, 70], cache.values[0][899, :, 9] = math.inf, math.nan, -math.inf
+    cache.store()
+    rb, rows = tc.rows_of([news, news])
+    q = queries(rows, 8, 4)
+    q[:, :, 0] = 1.0
+    before = [n - news for n in lens]
+    for call in (dict(window=(lens, 2000, 0)), dict(tree=([[0, 0]], [before], before, [2 ** 64 - 1] * rows))):
+        out, lse = run(cache, q, rb, bf16, ws=ws, **call)
+        assert bool((out[:news] == 0).all()) and bool((lse[:news] == -math.inf).all())
+        assert bool(torch.isfinite(out[news:]).all()) and bool(torch.isfinite(lse[news:]).all())
 
 
 # ---- counts and entries that do not fit together ----------------------------------------------------
