@@ -46,8 +46,9 @@ extern "C" {
  * an fp32 result the weights enter the product with the values to 24 bits, with a bf16 result rounded to
  * bf16.  The fp32 result and lse of several calls over disjoint tokens merge exactly with
  * bana_merge_partials (batch = rows).  A NaN or +inf among a row's scores makes the row NaN; a row whose
- * scores are all -inf gives 0 and -inf as one that sees nothing does.  What a row does not see never
- * reaches it, whatever its keys and values hold.
+ * scores are all -inf gives 0 and -inf as one that sees nothing does.  A value that is not finite gives the rows
+ * that see it, in its dim, what the formula gives: +-inf, or NaN for a NaN, both signs or a weight that is 0 in
+ * fp32.  What a row does not see never reaches it, whatever its keys and values hold.
  *   q           bf16 [rows][num_q_heads][128]
  *   kv_range_*  int32 [n_parts][batch], 1 <= n_parts <= 63
  *   tree_begin  int32 [batch]

@@ -1,5 +1,5 @@
-"""Calls on new tokens and blocks where the cache is unusual: scores that are not finite, counts and entries that do not
-fit together."""
+"""Calls on new tokens and blocks where the cache is unusual: scores and values that are not finite, counts and
+entries that do not fit together."""
 
 import math
 
@@ -70,6 +70,38 @@ def test_scores_of_minus_infinity_give_zero_whatever_the_values(news, bf16, ws):
         out, lse = run(cache, q, rb, bf16, ws=ws, **call)
         assert bool((out[:news] == 0).all()) and bool((lse[:news] == -math.inf).all())
         assert bool(torch.isfinite(out[news:]).all()) and bool(torch.isfinite(lse[news:]).all())
+
+
+@pytest.mark.parametrize("ws", [True, False])
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("news", [3, 60])  # tiles of 64 columns and of 128
+def test_infinite_values_that_rows_see(news, bf16, ws):
+    """What the definition gives, wherever the token lies: +-inf for one of them, NaN for both signs or a NaN; no other
+    dim, head or row is touched."""
+    lens = [700, 90]
+    rb, rows = tc.rows_of([news, min(news, 40)])
+    q = queries(rows, 8, 6)
+    for at in (3, 200, 401, 640, 698):  # blocks that all rows see whole, and blocks that they see in part
+        cache = tc.Cache(lens, 2, 5)
+        window = (lens, 650, 2)
+        clean, clean_lse = run(cache, q, rb, bf16, window=window, ws=ws)
+        cache.values[0][at, 0, 17] = math.inf
+        cache.values[0][at, 0, 18] = -math.inf
+        cache.values[0][at, 0, 19] = math.nan
+        cache.values[0][at, 0, 100], cache.values[0][at + 1, 0, 100] = math.inf, -math.inf
+        cache.store()
+        out, lse = run(cache, q, rb, bf16, window=window, ws=ws)
+        want = clean.clone()
+        pos = [700 - news + i for i in range(news)]
+        sees = [t <= p and (p - t < 650 or t < 2) for t in (at, at + 1) for p in pos]
+        one, other = torch.tensor(sees[:news]), torch.tensor(sees[news:])
+        first = want[:news, :4]  # the kv head's query heads
+        first[one, :, 17], first[one, :, 18], first[one, :, 19] = math.inf, -math.inf, math.nan
+        first[one & ~other, :, 100], first[~one & other, :, 100] = math.inf, -math.inf
+        first[one & other, :, 100] = math.nan
+        assert torch.equal(lse, clean_lse)
+        assert torch.equal(torch.isnan(out), torch.isnan(want)), at
+        assert torch.equal(torch.nan_to_num(out, 1e30), torch.nan_to_num(want, 1e30)), at
 
 
 # ---- counts and entries that do not fit together ----------------------------------------------------
