@@ -1,8 +1,9 @@
-"""Calls on new tokens and blocks where the cache is unusual: scores and values that are not finite, counts and
-entries that do not fit together."""
+"""Calls on new tokens and blocks where the cache or the batch is unusual: scores and values that are not finite, counts
+and entries that do not fit together, rows spread unevenly over many sequences."""
 
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -102,6 +103,36 @@ def test_infinite_values_that_rows_see(news, bf16, ws):
         assert torch.equal(lse, clean_lse)
         assert torch.equal(torch.isnan(out), torch.isnan(want)), at
         assert torch.equal(torch.nan_to_num(out, 1e30), torch.nan_to_num(want, 1e30)), at
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("nodes", [24, 12])  # tiles of 128 columns and of 64
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_rows_keep_their_bits_beside_values_that_they_do_not_see(bad, nodes, bf16):
+    """Nodes whose key or value is not finite: the rows that do not see them keep every bit of the result."""
+    cache = tc.Cache([50 + nodes], 2, 19)
+    rb, rows = tc.rows_of([nodes], pad=1, first=1)
+    q = queries(rows, 8, 20)
+    masks = [0] + [1 << i | (1 if i % 2 else 0) for i in range(nodes)] + [2 ** 64 - 1]
+    tree = ([[0]], [[50]], [50], masks)
+    clean, clean_lse = run(cache, q, rb, bf16, tree=tree)
+    cache.values[0][56] = bad
+    cache.keys[0][57] = bad
+    cache.values[0][57, 1, 5] = bad
+    cache.store()
+    out, lse = run(cache, q, rb, bf16, tree=tree)
+    other = [r for r in range(1, nodes + 1) if r - 1 not in (6, 7)]
+    assert torch.equal(out[other], clean[other]) and torch.equal(lse[other], clean_lse[other])
+    assert not torch.isfinite(out[7]).any()
+    cache = tc.Cache([100], 2, 23)
+    q, window = queries(2 * nodes, 8, 24), ([100], 20, 3)
+    clean, clean_lse = run(cache, q, [0, 2 * nodes], bf16, window=window)
+    cache.values[0][85] = bad
+    cache.store()
+    out, lse = run(cache, q, [0, 2 * nodes], bf16, window=window)
+    sees = torch.tensor([85 <= 100 - 2 * nodes + i < 105 for i in range(2 * nodes)])
+    assert torch.equal(out[~sees], clean[~sees]) and torch.equal(lse, clean_lse)
+    assert not torch.isfinite(out[sees]).any()
 
 
 # ---- counts and entries that do not fit together ----------------------------------------------------
@@ -223,3 +254,124 @@ def test_reserve_leaves_entries_that_are_not_minus_one():
     bana.bana_reserve_kv_blocks(p.table, p.lens, ints([64, 80, 32]), p.refs, p.status, p.ws)
     for x, y in zip(p.copy(), want):
         assert same(x, y)
+
+
+def test_race_check_build_on_unusual_inputs(monkeypatch):
+    """Infinite values in steps that all rows see whole (fp32 lists walked once more), and forks of blocks without
+    references, in the LDS race-check build: the same bits."""
+    def results():
+        found = []
+        for news in (3, 60):
+            cache = tc.Cache([700, 90], 2, 5)
+            cache.values[0][300, 0, 17], cache.values[0][20, 1, 3] = math.inf, math.nan
+            cache.store()
+            rb, rows = tc.rows_of([news, news])
+            found += run(cache, queries(rows, 8, 6), rb, False, window=([700, 90], 650, 2))
+        p = Blocks([40, 37, 500, 0, 0, 0, 0], 60, 33, 1)
+        p.refs[p.table[0, 1].long()] = p.refs[p.table[2, 31].long()] = 0
+        bana.bana_fork_kv_seqs(ints([0, 2, 1, 2]), ints([4, 6, 5, 3]), p.k, p.v, p.table, p.lens, p.refs, p.status, p.ws)
+        return found + p.copy()
+
+    want = results()
+    assert int(want[-1]) == 4
+    monkeypatch.setattr(bana, "_native", bana._PythonChecks())
+    monkeypatch.setattr(bana, "_lib", bana.load(bana.RACECHECK_LIB_PATH))
+    for x, y in zip(results(), want):
+        assert torch.equal(torch.isnan(x), torch.isnan(y)) and torch.equal(torch.nan_to_num(x), torch.nan_to_num(y))
+
+
+def test_captured_forks_replay():
+    """Two graphs of forks, each with a workspace of its own, one of blocks without references: every replay leaves what
+    the plain form leaves."""
+    pools = [Blocks([40, 37, 64, 0, 0, 0], 20, 4, 6), Blocks([33, 16, 9, 0, 0, 0], 20, 4, 7)]
+    pools[1].refs[pools[1].table[0, 0].long()] = pools[1].refs[pools[1].table[2, 0].long()] = 0
+    names = ("k", "v", "table", "lens", "refs", "status")
+    src, dst = [0, 2, 0], [5, 3, 4]
+    before = [[getattr(p, n).clone() for n in names] for p in pools]
+    want = [p.copy() for p in pools]
+    for x in want:
+        fork(src, dst, *x)
+    s, d, graphs = ints(src), ints(dst), []
+    for p in pools:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            bana.bana_fork_kv_seqs(s, d, p.k, p.v, p.table, p.lens, p.refs, p.status, p.ws)
+    for _ in range(4):
+        for p, old in zip(pools, before):
+            for n, x in zip(names, old):
+                getattr(p, n).copy_(x)
+            p.ws.fill_(0x7F)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for p, ref in zip(pools, want):
+            for x, y, n in zip(p.copy(), ref, names):
+                assert same(x, y), n
+    assert [int(p.status) for p in pools] == [0, 4]
+
+
+# ---- rows spread unevenly over many sequences -------------------------------------------------------
+
+def rounds_taken(row_begin, x, per_x, first):
+    """Rounds of the search for the last sequence b with first(b, row_begin[b]) <= x, 0 where the look at 64 neighbours
+    of its place among even sequences settles it."""
+    B = len(row_begin) - 1
+    starts = np.array([first(b, row_begin[b]) for b in range(B)])
+    near = min(max(int(np.float32(x) * np.float32(per_x)) - 31, 0), max(B - 63, 0))
+    ok = int((starts[near:near + 64] <= x).sum())
+    if B > 1 and ok < 64 and (ok > 0 or near == 0):
+        return 0
+    rounds, n = 0, B
+    while n > 1:
+        rounds, n = rounds + 1, -(-n // 64)
+    return rounds
+
+
+def skewed(B, where):
+    """Nearly all rows in one sequence; single rows before and behind it, most sequences without."""
+    at = {"first": 0, "middle": B // 2 + 3, "last": B - 1}[where]
+    news = [1 if b % 9 == 4 and abs(b - at) > 20 or abs(b - at) in (1, 3) else 0 for b in range(B)]
+    if B > 1000:
+        news = [n if b % 4 == 0 else 0 for b, n in enumerate(news)]
+    news[at] = 3000
+    return news
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("B,rounds", [(64, 1), (100, 2), (800, 2), (5000, 3)])
+def test_append_finds_the_sequences_of_uneven_batches(B, rounds, where):
+    news = skewed(B, where)
+    rb, rows = tc.rows_of(news, pad=5, first=3)
+    first = [(5 * b) % 23 for b in range(B)]
+    lens = [f + n if n else 0 for f, n in zip(first, news)]
+    cache = tc.Cache(lens, 1, 6)
+    places = rows // 16 + 2 * B
+    taken = {rounds_taken(rb, x, B / places, lambda b, row: row // 16 + 2 * b) for x in range(places)}
+    assert taken == ({0} if B <= 100 and where == "middle" else {0, rounds})  # few sequences: 64 neighbours are most
+    g = torch.Generator().manual_seed(7)
+    kr, vr = (torch.randn((rows, 1, tc.D), generator=g).to(torch.bfloat16) for _ in range(2))
+    k, v, table = cache.k.to(DEV), cache.v.to(DEV), cache.table.to(DEV)
+    tc.append(kr, vr, rb, first, cache.table, cache.k, cache.v)
+    bana.bana_append_kv(kr.to(DEV), vr.to(DEV), ints(rb), ints(first), table, k, v)
+    assert same(k, cache.k) and same(v, cache.v)
+
+
+@pytest.mark.parametrize("where", ["first", "middle", "last"])
+@pytest.mark.parametrize("B,rounds", [(100, 2), (800, 2), (5000, 3)])
+def test_attention_finds_the_sequences_of_uneven_batches(B, rounds, where):
+    news = skewed(B, where)
+    rb, rows = tc.rows_of(news, pad=5, first=3)
+    lens = [n + b % 7 if n else 0 for b, n in enumerate(news)]
+    cache = tc.Cache(lens, 1, 8)
+    hq, width = 4 if B == 100 else 2, 8
+    tile = 64 if rows * hq <= B * 64 else 128
+    slots = rows * hq // tile + B
+    taken = {rounds_taken(rb, x, B / slots, lambda b, row: row * hq // tile + b) for x in range(slots)}
+    assert taken == ({0} if B <= 100 and where == "middle" else {0, rounds})  # few sequences: 64 neighbours are most
+    q = queries(rows, hq, 9)
+    want = tc.attention(q, rb, cache, tc.window_sees(lens, news, width, 1), 0.0884)
+    out, lse = run(cache, q, rb, False, window=(lens, width, 1))
+    live = slice(rb[0], rb[-1])
+    tc.check_attention(out[live], lse[live], (want[0][live], want[1][live], tuple(x[live] for x in want[2])), False)
+    for part in (slice(0, rb[0]), slice(rb[-1], None)):
+        assert bool((out[part] == 7.0).all()) and bool((lse[part] == 7.0).all())
