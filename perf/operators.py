@@ -286,7 +286,7 @@ def _run_own(s):
         return [s["k"], s["v"]]
     if op in ("tree", "window"):
         if "dims" not in s:  # the lengths that a serving program knows on the host
-            live = s["lens"] if op == "tree" else s["lens"] + s["news"]
+            live = s["lens"] + s["news"]
             s["dims"] = bana.make_dims(case["batch"], case["hq"], case["hkv"], s["table"].shape[1], s["k"].shape[0],
                                        max_range_tokens=int(live.max()), total_range_tokens=int(live.sum()))
         rows, scale = s["q"].shape[0], D ** -0.5
