@@ -13,7 +13,8 @@
  * return before any HIP call.  Pools, block tables and bana_dims are those of bana.h.  Of bana_dims
  * these calls read the shapes and, as hints for the attention, max_range_tokens (the most cached
  * tokens of a sequence, new ones included) and total_range_tokens (their sum over sequences); the other
- * hints must be valid and are ignored.  Values that live on the device are not checked on the host,
+ * hints must be valid and are ignored.  Without max_range_tokens the attention is split over workgroups for
+ * sequences as long as the table: much shorter ones are split less, or not at all.  Values that live on the device are not checked on the host,
  * but no value makes a call read or write outside the buffers it was given: offsets outside the rows, the
  * table or the pool are clamped or skipped.  A wrong value gives wrong results, not a fault.
  *
@@ -48,7 +49,8 @@ extern "C" {
  * bana_merge_partials (batch = rows).  A NaN or +inf among a row's scores makes the row NaN; a row whose
  * scores are all -inf gives 0 and -inf as one that sees nothing does.  A value that is not finite gives the rows
  * that see it, in its dim, what the formula gives: +-inf, or NaN for a NaN, both signs or a weight that is 0 in
- * fp32.  What a row does not see never reaches it, whatever its keys and values hold.
+ * fp32.  (The sums are of weights up to 2^8: finite values below 2^90 never overflow them.)  What a row does not
+ * see never reaches it, whatever its keys and values hold.
  *   q           bf16 [rows][num_q_heads][128]
  *   kv_range_*  int32 [n_parts][batch], 1 <= n_parts <= 63
  *   tree_begin  int32 [batch]
@@ -89,7 +91,8 @@ size_t bana_window_attn_workspace_bytes(const bana_dims* d, int64_t rows, int32_
 /*
  * Keys and values of new tokens into the cache: row row_begin[b] + i becomes token first_token[b] + i of
  * sequence b, bit for bit.  Rows whose token lies outside the table, or whose table entry names no block of the pool,
- * are skipped.  Two rows of one call must not name the same slot.  Of d, num_q_heads is not used.
+ * are skipped.  Two rows of one call must not name the same slot, and the blocks written must belong to one sequence
+ * only: a whole block that a fork shares stays shared when a release cuts into it.  Of d, num_q_heads is not used.
  * BANA_ERR_UNSUPPORTED: rows as above, batch * num_kv_heads above 2^18.
  *   k_rows, v_rows  bf16 [rows][num_kv_heads][128]
  */

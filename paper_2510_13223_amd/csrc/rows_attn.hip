@@ -286,14 +286,17 @@ __device__ __forceinline__ void store_row(void* __restrict__ out, float* __restr
 // rounded to bf16, half a step of the result's own type; an fp32 result takes them as three bf16 terms, 24 bits.
 // Their sum is of the unrounded ones in both.
 //
-// What bounds it, 32 columns: the matrix and vector units, at the clock that the card's power leaves them.  A step of
+// What bounds it, 32 columns: the matrix and vector units, at the clock that the card's power leaves them (1.8 GHz; the
+// matrix units are busy half of its cycles).  A step of
 // a wavefront is 16 matrix instructions of 32 cycles, some 80 vector instructions and 16 exponentials, and 16 KiB of
 // LDS reads; three workgroups on a CU overlap them in part.  2 x 4096 new tokens, 32 heads, window 4096, bf16: 537 to
 // 560 us, 1.0 PFLOP/s, where a library product of 8192^3 reaches 1.47; the same call on zeros takes 425.  Without the
 // weights' computation 444, with one LDS fragment for all 498, without both 401.  32 trees of 64 nodes over 8000
 // tokens, 64 heads: 597 to 620 us.  Instructions of 16 x 16 x 32 for 32 columns: 2 % more; 64 columns a wavefront, one
 // per SIMD, with the next step's scores before this step's values, were slower (the registers of two steps spill).
-// 16 columns: HBM.  64 single tokens, window 4096: 168 us, 6.4 TB/s.
+// At three workgroups on a CU the bf16 kernels spill 5 registers (window) or 9 (tree); a masked step reads one back, and
+// its wait takes in the requests under way.
+// 16 columns: HBM.  64 single tokens, window 4096: 169 us, 6.4 TB/s.
 constexpr int kTileBytes = kTileElems * 2;
 constexpr int kKStep = 2 * kTileBytes + 128;    // K tiles of a step, the second 64 bytes off
 constexpr int kVStep = 2 * kTileBytes;

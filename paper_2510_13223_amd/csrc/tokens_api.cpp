@@ -89,7 +89,8 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
 
 // How a call's tiles are cut.  A tile is 128 columns (rows x heads of a group), or 64 where sequences have no more
 // on the mean: four wavefronts of 16 columns then share what two of 32 would do one after the other (24 drafts of
-// 13 nodes, groups of 4, fp32: 106 -> 71 us), and the loads go past the caches, as no other tile reads them.
+// 13 nodes, groups of 4, fp32: 106 -> 71 us), and the loads go past the caches, as most sequences then have one tile (of
+// those drafts some have two that read the same context, and it is 76 us so, 78 otherwise).
 //
 // A tile's list of steps (32 tokens) is cut into chunks where that is estimated to be faster.  With n
 // workgroups at work, of at most `slots`, a step takes max(latency, n x step_us): alone it is bound by the chain of
@@ -101,6 +102,9 @@ bana::RowsAttnArgs attention_args(const bana_dims* d, int64_t rows, const int32_
 // Calls that fixed the rule, one chunk -> as planned: 8 rows over 700 tokens 34 -> 11.8; 64 rows, window 4096, 178
 // -> 168; 1 row over 16000 tokens 211 -> 18.5; 2048 rows x 64 heads, 3200 to 12800 tokens, 646 -> 618; prompts of 750
 // rows, window 512, stay whole (46, in two chunks 83).
+//
+// A chunk is never shorter than planned for the longest list, so that short lists do not make many.  Without the
+// hint max_range_tokens that is the table's span, and a list far below it stays in one chunk.
 struct RowsPlan {
   int nc = 1;
   int least = 1;  // steps of a chunk at least
