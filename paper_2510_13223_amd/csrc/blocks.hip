@@ -7,7 +7,7 @@
 //
 // Bound by the latency of dependent reads, not by their bytes: lengths, table entries, counts, list, each a round trip
 // of some 0.7 us, and two launches for a fork.  Measured on MI355X: blocks for 128 drafts of 64 tokens, pool of
-// 116,000, 8.6 us; 96 forks of 1500 tokens, 8 kv heads, and their release, 15.6 us.
+// 116,000, 8.6 us; 96 forks of 1500 tokens, 8 kv heads, and their release, 15.4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -221,7 +221,7 @@ __device__ __forceinline__ void for_source_blocks(int n, G fork, const int32_t* 
 // The counts of the blocks that the sources name are judged before any changes: one without references is left alone by
 // the forks (ws[1] tells them to look; looking always would cost the next kernel 9 us, as loads of the counts then meet
 // the atomics on them) and is no free block of this call, whatever its count.  96 forks of 32 sequences of 1500 tokens:
-// 8.8 us, without the walk over the sources' entries 5.4; with 16 entries to a thread 9.4, most of that more code to fetch.
+// 8.6 us, without the walk over the sources' entries 5.4; with 16 entries to a thread 9.4, most of that more code to fetch.
 __global__ __launch_bounds__(kPlanThreads) void fork_plan_kernel(const int32_t* __restrict__ src,
                                                                  const int32_t* __restrict__ dst, int n,
                                                                  const int32_t* __restrict__ table,
