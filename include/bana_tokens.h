@@ -13,10 +13,11 @@
  * return before any HIP call.  Pools, block tables and bana_dims are those of bana.h.  Of bana_dims
  * these calls read the shapes and, as hints for the attention, max_range_tokens (the most cached
  * tokens of a sequence, new ones included) and total_range_tokens (their sum over sequences); the other
- * hints must be valid and are ignored.  Without max_range_tokens the attention is split over workgroups for
- * sequences as long as the table: much shorter ones are split less, or not at all.  Values that live on the device are not checked on the host,
- * but no value makes a call read or write outside the buffers it was given: offsets outside the rows, the
- * table or the pool are clamped or skipped.  A wrong value gives wrong results, not a fault.
+ * hints must be valid and are ignored.  Without max_range_tokens the attention is split over workgroups
+ * for sequences as long as the table: much shorter ones are split less, or not at all.  Values that live on
+ * the device are not checked on the host, but no value makes a call read or write outside the buffers it
+ * was given: offsets outside the rows, the table or the pool are clamped or skipped.  A wrong value gives
+ * wrong results, not a fault.
  *
  * Packed rows.  The new tokens of a batch are rows of dense arrays: sequence b has the rows
  * [row_begin[b], row_begin[b + 1]), n_b of them (possibly none); row_begin is int32 [batch + 1] and
